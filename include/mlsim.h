@@ -410,6 +410,116 @@ int sim_static_run_generated(const sim_static *st, int64_t n_scen, const int32_t
                              int64_t scen0, int32_t *makespan, int32_t *finish, int64_t ld_fin,
                              int32_t *status, void *stream);
 
+/*
+ * Placement policies.  A search over placements keeps, for every op, logits
+ * over the resources; it draws the placements of a batch of scenarios from
+ * them, replays the batch, and moves the logits by what the replay said.  A
+ * sim_policy names the logits of n_pol policies and which scenario belongs to
+ * which:
+ *   logits      device [n_pol][n_ops][n_res] of `dtype` (resources contiguous):
+ *               op v under policy p begins at element p * ld_pol + v * ld_op.
+ *               Strides of 0 share rows.  -inf: the op may not run there.
+ *   n_ops, n_res  within the limits of sim_graph_create; n_pol >= 1.
+ *   block, scen0  global scenario S = scen0 + s belongs to policy
+ *               (S / block) mod n_pol; block >= 1, scen0 >= 0.
+ *   temperature, top_k, top_p, min_p   the settings of every policy, or
+ *   settings    device float32 [n_pol][4]: those four for each policy (top_k
+ *               as a number); the fields above are then not read.
+ * Settings: a temperature T >= 0 (finite); top_k >= 0 (0: all); top_p and
+ * min_p in [0, 1] (1 and 0: all).  Out of range, the fields return
+ * SIM_E_INVAL; an entry of the device array makes its policy's rows invalid.
+ * The struct is host memory, read during the call only.  At most
+ * SIM_MAX_POLICY_SCEN scenarios a call.
+ *
+ * With w_r = exp((l_r - max l) / T), the probability of resource r is
+ * w_r / sum w.  A row (the logits of one op and policy) that holds NaN or +inf
+ * or has invalid settings is invalid; a row of -inf only is empty.
+ *
+ * Every call returns SIM_E_INVAL or SIM_E_LIMIT before anything is enqueued,
+ * is asynchronous on `stream`, allocates nothing and gives the same bits every
+ * time.  Sums are held in at least 32 bits.
+ */
+#define SIM_MAX_POLICY_SCEN (INT64_C(1) << 40)
+enum { SIM_F32 = 0, SIM_BF16 = 1, SIM_F16 = 2 };
+typedef struct sim_policy {
+  const void *logits;
+  int64_t ld_pol, ld_op;
+  int64_t block, scen0;
+  const float *settings;
+  float temperature;
+  int32_t top_k;
+  float top_p, min_p;
+  int32_t dtype;
+  int32_t n_pol, n_ops, n_res;
+} sim_policy;
+
+/*
+ * Draw a placement for every scenario from given random numbers.
+ *   u      device float32 [n_ops][ld_u], ld_u >= n_scen, in [0, 1).
+ *   place  device uint16 [n_ops][ld_place], ld_place >= n_scen: as
+ *          sim_run_batch reads it.
+ * Order a row's resources with a finite logit by falling logit, equal ones by
+ * rising index.  Kept are the first top_k of the order; of them those before
+ * which less than top_p of their mass lies (always the first); of them those
+ * with w_r >= min_p (always the first).  C_r is the sum of the kept w up to
+ * resource r, by index; place = the lowest kept r with C_r > u * C_(n_res - 1),
+ * computed as in 64 bits.  T = 0 takes the first of the order.  u below 0 acts
+ * as 0, u >= 1 takes the last resource of positive weight.  An empty or
+ * invalid row, or u NaN, gives 65535, which the replay reports as
+ * SIM_ST_BAD_RES.
+ */
+int sim_policy_sample(const sim_policy *p, int64_t n_scen, const float *u, int64_t ld_u,
+                      uint16_t *place, int64_t ld_place, void *stream);
+
+/*
+ * logp[s] (device float32 [n_scen]) = the sum over the ops of the logarithm of
+ * the probability of place[v][s] in its row (top_k, top_p and min_p are not
+ * read).  -inf where an op's place is >= n_res or its logit -inf (every place
+ * of an empty row); NaN where a row is invalid or T = 0.
+ *   work, work_bytes  device scratch of at least sim_policy_work bytes (the same
+ *          for logp and grad; 0: may be NULL), aligned to 8, for this call alone
+ *          until it has run.
+ */
+int64_t sim_policy_work(const sim_policy *p, int64_t n_scen); /* bytes, or a negative SIM_E_* code */
+int sim_policy_logp(const sim_policy *p, int64_t n_scen, const uint16_t *place, int64_t ld_place,
+                    float *logp, void *work, int64_t work_bytes, void *stream);
+
+/*
+ * The gradient of sum_s weight[s] * logp[s] with respect to the logits:
+ *   grad[p][v][r] = (h_r - W w_r / sum w) / T,
+ * h_r the sum of weight[s] over the policy's scenarios with place[v][s] = r,
+ * W the sum of the row's h_r; 0 where the logit is -inf.  A place >= n_res or
+ * on a logit of -inf adds nothing.  Invalid rows and T = 0 give NaN.
+ *   weight  device float32 [n_scen].
+ *   grad    device [n_pol][n_ops][n_res] of `dtype`, written whole: strides
+ *           ld_gpol and ld_gop in elements, no row over another.
+ *   work    as sim_policy_logp.
+ */
+int sim_policy_grad(const sim_policy *p, int64_t n_scen, const uint16_t *place, int64_t ld_place,
+                    const float *weight, void *grad, int64_t ld_gpol, int64_t ld_gop, void *work,
+                    int64_t work_bytes, void *stream);
+
+/*
+ * Distil another policy's best resources into this one.  The teacher names
+ * `top` resources for every row and their logits (of `dtype`):
+ *   top_res     device uint16, entry k of op v under policy p at
+ *               p * ld_res_pol + v * ld_res_op + k; >= n_res: no entry.
+ *   top_logits  device, the same with ld_log_pol and ld_log_op; -inf: no entry.
+ *   top         1 .. SIM_MAX_RES.
+ * q = the softmax of the entries' logits / T, added up by resource (one may be
+ * named twice); loss[p][v] (device float32 [n_pol][n_ops]) =
+ * sum_r q_r log(q_r / pi_r), pi the row's probabilities; grad (or NULL; as
+ * above) = weight[p][v] (pi_r - q_r) / T, 0 where the logit is -inf, weight
+ * device float32 [n_pol][n_ops] or NULL for 1.  A row without entries has loss
+ * and gradient 0.  Where the teacher names a resource whose logit is -inf the
+ * loss is +inf.  Invalid rows, T = 0 and NaN or +inf among a row's entries give
+ * NaN.  block, scen0, top_k, top_p and min_p are checked but not used.
+ */
+int sim_policy_distill(const sim_policy *p, const uint16_t *top_res, int64_t ld_res_pol,
+                       int64_t ld_res_op, const void *top_logits, int64_t ld_log_pol,
+                       int64_t ld_log_op, int32_t top, const float *weight, float *loss,
+                       void *grad, int64_t ld_gpol, int64_t ld_gop, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

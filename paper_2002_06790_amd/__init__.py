@@ -36,14 +36,27 @@ EXPORTS = ("sim_graph_create", "sim_graph_destroy", "sim_run_batch", "sim_critic
            "sim_static_destroy", "sim_static_run", "sim_attribute", "sim_generate", "sim_run_generated",
            "sim_critical_path_generated", "sim_run_batch_gap", "sim_static_run_generated",
            "sim_run_batch_dev", "sim_run_batch_share", "sim_run_batch_noalloc", "sim_testing_sweep_table",
-           "sim_testing_join_slots", "sim_testing_merge_program")
+           "sim_testing_join_slots", "sim_testing_merge_program", "sim_policy_sample", "sim_policy_work",
+           "sim_policy_logp", "sim_policy_grad", "sim_policy_distill")
 
 #: generator limits (include/mlsim.h): largest base duration, noise bound
 SIM_GEN_BASE_MAX, SIM_GEN_NOISE_MAX = 1 << 24, 1 << 20
 #: relative standard deviation of the generated noise per unit of ``noise``
 GEN_SIGMA_UNIT = 2.0 * (2.0 * (65536.0**2 - 1.0) / 3.0) ** 0.5 / 2.0**40
 
+#: placement drawn from a row without a valid distribution (include/mlsim.h)
+NO_PLACE = 65535
+
 _lib = None
+
+
+class _PolicyStruct(ctypes.Structure):
+    """sim_policy (include/mlsim.h)."""
+    _fields_ = [("logits", ctypes.c_void_p), ("ld_pol", ctypes.c_int64), ("ld_op", ctypes.c_int64),
+                ("block", ctypes.c_int64), ("scen0", ctypes.c_int64), ("settings", ctypes.c_void_p),
+                ("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float), ("dtype", ctypes.c_int32), ("n_pol", ctypes.c_int32),
+                ("n_ops", ctypes.c_int32), ("n_res", ctypes.c_int32)]
 
 
 class SimError(RuntimeError):
@@ -115,6 +128,17 @@ def _load():
     L.sim_testing_join_slots.restype = ctypes.c_int
     L.sim_testing_merge_program.argtypes = [I32, I32, P, P, P, P, I32, P, P, I64, P, I64, P, I64]
     L.sim_testing_merge_program.restype = ctypes.c_int
+    PS = ctypes.POINTER(_PolicyStruct)
+    L.sim_policy_sample.argtypes = [PS, I64, P, I64, P, I64, P]
+    L.sim_policy_sample.restype = ctypes.c_int
+    L.sim_policy_work.argtypes = [PS, I64]
+    L.sim_policy_work.restype = I64
+    L.sim_policy_logp.argtypes = [PS, I64, P, I64, P, P, I64, P]
+    L.sim_policy_logp.restype = ctypes.c_int
+    L.sim_policy_grad.argtypes = [PS, I64, P, I64, P, P, I64, I64, P, I64, P]
+    L.sim_policy_grad.restype = ctypes.c_int
+    L.sim_policy_distill.argtypes = [PS, P, I64, I64, P, I64, I64, I32, P, P, P, I64, I64, P]
+    L.sim_policy_distill.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -299,6 +323,209 @@ def _stream_ptr(stream):
     return s.cuda_stream
 
 
+def _dev_rows(t, dtype, shape, device, what):
+    """(pointer, policy stride, op stride) of a [n_pol, n_ops, k] device tensor
+    with unit stride along its last dimension."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a torch tensor on the GPU")
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be {dtype} of shape {shape}, not {t.dtype} of {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, the logits on {device}")
+    if shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{what} must have unit stride along its last dimension")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+class Policy:
+    """Placement policies: logits over the resources for every op
+    (sim_policy, include/mlsim.h).
+
+    ``logits``: float32, bfloat16 or float16 tensor [n_pol, n_ops, n_res] (or
+    [n_ops, n_res]: one policy) on the GPU, contiguous along the resources; its
+    other strides are free, so an expanded tensor shares rows.  It is kept, not
+    copied: updates in place take effect.  -inf: the op may not run there.
+    Global scenario S belongs to policy ``(S // block) % n_pol``; ``scen0`` is
+    the global index of a call's first scenario.
+
+    ``temperature``, ``top_k`` (0: all), ``top_p`` and ``min_p``: numbers, or
+    one per policy as a sequence or tensor (rounded to float32).  Only
+    ``sample`` reads the last three.
+
+    Calls run on ``stream`` (default: the current stream of the logits'
+    device), are asynchronous and may be captured into a graph.  Gradients come
+    back as tensors: ``logits.backward(policy.grad(...))`` hands them on to a
+    network that made the logits.
+    """
+
+    def __init__(self, logits, block: int = 1, scen0: int = 0, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+        import torch
+        if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+            raise TypeError("logits must be a torch tensor on the GPU")
+        codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        if logits.dtype not in codes:
+            raise TypeError(f"logits must be float32, bfloat16 or float16, not {logits.dtype}")
+        self.logits = logits = logits.detach()
+        if logits.dim() == 2:
+            logits = logits[None]
+        if logits.dim() != 3:
+            raise ValueError("logits must have shape (n_pol, n_ops, n_res) or (n_ops, n_res)")
+        self.n_pol, self.n_ops, self.n_res = (int(x) for x in logits.shape)
+        if self.n_res > 1 and logits.stride(2) != 1:
+            raise ValueError("logits must have unit stride along the resources")
+        self.device = logits.device
+        values = (temperature, top_k, top_p, min_p)
+        self.settings = None
+        if not all(isinstance(x, (int, float)) for x in values):
+            rows = []
+            for name, x in zip(("temperature", "top_k", "top_p", "min_p"), values):
+                x = torch.as_tensor(x, dtype=torch.float32).detach().to(self.device)
+                if x.dim() > 1 or (x.dim() == 1 and x.numel() != self.n_pol):
+                    raise ValueError(f"{name} must be a number or one per policy ({self.n_pol})")
+                rows.append(x.expand(self.n_pol))
+            self.settings = torch.stack(rows, 1).contiguous()
+            values = (1.0, 0, 1.0, 0.0)
+        elif int(top_k) != top_k:
+            raise ValueError("top_k must be a whole number")
+        self._c = _PolicyStruct(logits.data_ptr(), logits.stride(0), logits.stride(1), int(block), int(scen0),
+                                None if self.settings is None else self.settings.data_ptr(), values[0],
+                                int(values[1]), values[2], values[3], codes[logits.dtype], self.n_pol, self.n_ops,
+                                self.n_res)
+        rc = _load().sim_policy_work(self._c, 1)  # checks the policy itself, on the host
+        if rc < 0:
+            raise SimError(rc, "sim_policy")
+
+    def _on(self, stream, *inputs):
+        """The stream of a call, and the context in which it allocates and
+        launches.  Inputs of other streams are kept until it has run."""
+        import torch
+        cur = torch.cuda.current_stream(self.device)
+        if stream is None or stream == cur:
+            return cur, torch.cuda.device(self.device)
+        if stream.device != self.device:
+            raise ValueError(f"stream is on {stream.device}, the logits on {self.device}")
+        for t in (self.logits, self.settings, *inputs):
+            if t is not None:
+                t.record_stream(stream)
+        return stream, torch.cuda.stream(stream)
+
+    def _place(self, place, what="place"):
+        import torch
+        ptr, ld = _dev_matrix(place, torch.uint16, self.n_ops, what)
+        if place is None or place.device != self.device:
+            raise ValueError(f"{what} must be on {self.device}")
+        return ptr, ld, int(place.shape[1])
+
+    def _work(self, n_scen):
+        import torch
+        need = _load().sim_policy_work(self._c, n_scen)
+        if need < 0:
+            raise SimError(need, "sim_policy_work")
+        return (torch.empty(need // 8, dtype=torch.float64, device=self.device), need) if need else (None, 0)
+
+    def sample(self, u, out=None, stream=None):
+        """Draw placements from the random numbers ``u`` (float32 [n_ops, S] in
+        [0, 1)): uint16 [n_ops, S], for ``Graph.run(place=...)``
+        (sim_policy_sample).  A row without a valid distribution gives
+        ``NO_PLACE``, which the replay reports as SIM_ST_BAD_RES."""
+        import torch
+        uptr, ld = _dev_matrix(u, torch.float32, self.n_ops, "u")
+        if u is None or u.device != self.device:
+            raise ValueError(f"u must be on {self.device}")
+        S = int(u.shape[1])
+        st, ctx = self._on(stream, u, out)
+        with ctx:
+            if out is None:
+                out = torch.empty((self.n_ops, S), dtype=torch.uint16, device=self.device)
+            optr, ldo, So = self._place(out, "out")
+            if So < S:
+                raise ValueError(f"out must hold {S} scenarios")
+            rc = _load().sim_policy_sample(self._c, S, uptr, ld, optr, ldo, st.cuda_stream)
+        if rc:
+            raise SimError(rc, "sim_policy_sample")
+        return out
+
+    def logp(self, place, out=None, stream=None):
+        """Log-probability of every scenario's placement, float32 [S]: the sum
+        over the ops (sim_policy_logp)."""
+        import torch
+        pptr, ld, S = self._place(place)
+        st, ctx = self._on(stream, place, out)
+        with ctx:
+            if out is None:
+                out = torch.empty(S, dtype=torch.float32, device=self.device)
+            elif out.dtype != torch.float32 or out.dim() != 1 or out.numel() < S or out.device != self.device or \
+                    (S > 1 and out.stride(0) != 1):
+                raise ValueError(f"out must be float32 of shape ({S},) or longer, contiguous, on {self.device}")
+            work, need = self._work(S)
+            rc = _load().sim_policy_logp(self._c, S, pptr, ld, out.data_ptr(), work.data_ptr() if need else None,
+                                         need, st.cuda_stream)
+        if rc:
+            raise SimError(rc, "sim_policy_logp")
+        return out
+
+    def grad(self, place, weight, out=None, stream=None):
+        """The gradient of ``(weight * logp(place)).sum()`` with respect to the
+        logits, of their shape and type (sim_policy_grad).  ``weight``: float32
+        [S], for a policy gradient the advantage of every scenario's makespan."""
+        import torch
+        pptr, ld, S = self._place(place)
+        if not isinstance(weight, torch.Tensor) or not weight.is_cuda:
+            raise TypeError("weight must be a torch tensor on the GPU")
+        if weight.dtype != torch.float32 or tuple(weight.shape) != (S,) or weight.device != self.device or \
+                (S > 1 and weight.stride(0) != 1):
+            raise ValueError(f"weight must be float32 of shape ({S},), contiguous, on {self.device}")
+        st, ctx = self._on(stream, place, weight, out)
+        with ctx:
+            out, g = self._grad_out(out)
+            work, need = self._work(S)
+            rc = _load().sim_policy_grad(self._c, S, pptr, ld, weight.data_ptr(), *g,
+                                         work.data_ptr() if need else None, need, st.cuda_stream)
+        if rc:
+            raise SimError(rc, "sim_policy_grad")
+        return out
+
+    def _grad_out(self, out):
+        import torch
+        if out is None:
+            out = torch.empty(self.logits.shape, dtype=self.logits.dtype, device=self.device)
+        rows = out[None] if isinstance(out, torch.Tensor) and out.dim() == 2 else out
+        return out, _dev_rows(rows, self.logits.dtype, (self.n_pol, self.n_ops, self.n_res), self.device, "grad")
+
+    def distill(self, top_res, top_logits, weight=None, want_grad: bool = True, loss=None, grad=None, stream=None):
+        """Distil a teacher's best resources (sim_policy_distill): uint16
+        ``top_res`` [n_pol, n_ops, K] (n_res or more, as ``NO_PLACE``: no entry)
+        and their ``top_logits`` of the logits' type.  Returns ``(loss, grad)``:
+        the rows' divergence, float32 [n_pol, n_ops], and the gradient of
+        ``(weight * loss).sum()`` of the logits' shape and type (None unless
+        ``want_grad``); ``weight`` is float32 [n_pol, n_ops] or None for ones."""
+        import torch
+        if isinstance(top_res, torch.Tensor) and top_res.dim() == 2:
+            top_res = top_res[None]
+        if isinstance(top_logits, torch.Tensor) and top_logits.dim() == 2:
+            top_logits = top_logits[None]
+        K = int(top_res.shape[2]) if isinstance(top_res, torch.Tensor) and top_res.dim() == 3 else 0
+        res = _dev_rows(top_res, torch.uint16, (self.n_pol, self.n_ops, K), self.device, "top_res")
+        log = _dev_rows(top_logits, self.logits.dtype, (self.n_pol, self.n_ops, K), self.device, "top_logits")
+        for t, what in ((weight, "weight"), (loss, "loss")):
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (self.n_pol, self.n_ops) or
+                                  t.device != self.device or not t.is_contiguous()):
+                raise ValueError(f"{what} must be float32 of shape ({self.n_pol}, {self.n_ops}), contiguous, on {self.device}")
+        st, ctx = self._on(stream, top_res, top_logits, weight, loss, grad)
+        with ctx:
+            if loss is None:
+                loss = torch.empty((self.n_pol, self.n_ops), dtype=torch.float32, device=self.device)
+            g = (None, 0, 0)
+            if want_grad:
+                grad, g = self._grad_out(grad)
+            rc = _load().sim_policy_distill(self._c, *res, *log, K, None if weight is None else weight.data_ptr(),
+                                            loss.data_ptr(), *g, st.cuda_stream)
+        if rc:
+            raise SimError(rc, "sim_policy_distill")
+        return loss, grad if want_grad else None
+
+
 class Graph:
     """A compiled dataflow graph on the current HIP device (sim_graph_create)."""
 
@@ -402,6 +629,21 @@ class Graph:
             if rc:
                 raise SimError(rc, "sim_run_batch_gap")
         return makespan, finish, status
+
+    def run_sampled(self, policy: Policy, dur, u, want_finish: bool = False, algo: str = "auto", place=None,
+                    stream=None, gap=None, delay=None):
+        """Draw a placement for every scenario column of ``dur`` from
+        ``policy`` and the random numbers ``u`` (float32 [n_ops, S]) and replay
+        them (sim_policy_sample, then as ``run``).  Returns ``(makespan, finish
+        or None, status, place)``."""
+        if policy.n_ops != self.n_ops or policy.n_res != self.n_res:
+            raise ValueError(f"the policy is for {policy.n_ops} ops on {policy.n_res} resources, the graph has "
+                             f"{self.n_ops} on {self.n_res}")
+        if tuple(u.shape) != tuple(dur.shape):
+            raise ValueError(f"u must have dur's shape {tuple(dur.shape)}")
+        place = policy.sample(u, out=place, stream=stream)
+        return (*self.run(dur, place=place, want_finish=want_finish, algo=algo, stream=stream, gap=gap,
+                          delay=delay), place)
 
     def run_share(self, dur, share, want_finish: bool = False, makespan=None, finish=None, status=None,
                   stream=None):

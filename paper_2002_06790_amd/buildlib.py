@@ -9,12 +9,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libmlsim.so")
 SOURCES = ["csrc/graph.cpp", "csrc/api.cpp", "csrc/static.cpp", "csrc/pool.cpp", "csrc/merge.cpp", "csrc/kernels.hip",
-           "csrc/merge.hip", "csrc/share.hip"]
+           "csrc/merge.hip", "csrc/share.hip", "csrc/policy.cpp", "csrc/policy.hip"]
 ARCH = os.environ.get("MLSIM_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          f"--offload-arch={ARCH}",
-         # packed FP32 instructions stay off (this library has no FP32 math)
+         # packed FP32 instructions stay off
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
 

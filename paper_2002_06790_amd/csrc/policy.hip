@@ -1,0 +1,700 @@
+// Placement policies: rows of logits over resources, one row per op and
+// policy.  A group of G lanes holds a row, NV consecutive resources a lane, so
+// that up to eight rows share a wavefront and the sums within a row take
+// log2 G exchanges.
+#include <algorithm>
+#include <climits>
+
+#include "policy.hpp"
+#include "sim.hpp"
+
+namespace mlsim {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kInf = __builtin_inff();
+constexpr uint16_t kNoPlace = 65535;
+
+// ---- values across the lanes of a group (xor partners stay inside it) ----
+
+template <int G>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = 1; o < G; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+template <int G, class F>
+__device__ __forceinline__ F group_sum(F v) {
+#pragma unroll
+  for (int o = 1; o < G; o <<= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+template <int G>
+__device__ __forceinline__ uint32_t group_umax(uint32_t v) {
+#pragma unroll
+  for (int o = 1; o < G; o <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+  return v;
+}
+
+template <int G>
+__device__ __forceinline__ uint32_t group_umin(uint32_t v) {
+#pragma unroll
+  for (int o = 1; o < G; o <<= 1) v = min(v, (uint32_t)__shfl_xor((int)v, o));
+  return v;
+}
+
+// Sum over the lanes before this one, and over all of them.
+template <int G, class F>
+__device__ __forceinline__ F group_before(F v, int g, F &all) {
+  F in = v;
+#pragma unroll
+  for (int o = 1; o < G; o <<= 1) {
+    const F t = __shfl_up(in, o, G);
+    if (g >= o) in += t;
+  }
+  all = __shfl(in, G - 1, G);
+  const F ex = __shfl_up(in, 1, G);
+  return g ? ex : F(0);
+}
+
+// ---- rows ----
+
+__device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
+__device__ __forceinline__ float f16_value(uint32_t bits) {
+  const uint16_t b = (uint16_t)bits;
+  _Float16 h;
+  __builtin_memcpy(&h, &b, 2);
+  return (float)h;
+}
+// Round to nearest, ties to even; NaN stays NaN.
+__device__ __forceinline__ uint32_t bf16_bits(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return x != x ? 0x7FC0u : (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
+}
+__device__ __forceinline__ uint32_t f16_bits(float x) {
+  const _Float16 h = (_Float16)x;
+  uint16_t b;
+  __builtin_memcpy(&b, &h, 2);
+  return b;
+}
+__device__ __forceinline__ float half_value(uint32_t bits, bool f16) { return f16 ? f16_value(bits) : bf16_value(bits); }
+
+__device__ __forceinline__ float load_elem(const void *base, int32_t dtype, int64_t i) {
+  if (dtype == SIM_F32) return ((const float *)base)[i];
+  return half_value(((const uint16_t *)base)[i], dtype == SIM_F16);
+}
+
+// x[j] = the row's element r0 + j, -inf behind its end.
+template <int NV>
+__device__ __forceinline__ void load_row(const void *base, int32_t dtype, int64_t row, int r0, int n, bool vec,
+                                         float (&x)[NV]) {
+  if (dtype == SIM_F32) {
+    const float *p = (const float *)base + row + r0;
+    if (vec && r0 + NV <= n) {
+#pragma unroll
+      for (int j = 0; j < NV; j += 4) {
+        const float4 t = *(const float4 *)(p + j);
+        x[j] = t.x, x[j + 1] = t.y, x[j + 2] = t.z, x[j + 3] = t.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) x[j] = r0 + j < n ? p[j] : -kInf;
+    }
+    return;
+  }
+  const uint16_t *p = (const uint16_t *)base + row + r0;
+  const bool f16 = dtype == SIM_F16;
+  if (vec && r0 + NV <= n) {
+#pragma unroll
+    for (int j = 0; j < NV; j += 8) {
+      const uint4 t = *(const uint4 *)(p + j);
+      const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[j + i] = half_value((w[i / 2] >> (16 * (i & 1))) & 0xFFFFu, f16);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) x[j] = r0 + j < n ? half_value(p[j], f16) : -kInf;
+  }
+}
+
+template <int NV>
+__device__ __forceinline__ void store_row(void *base, int32_t dtype, int64_t row, int r0, int n, bool vec,
+                                          const float (&x)[NV]) {
+  if (dtype == SIM_F32) {
+    float *p = (float *)base + row + r0;
+    if (vec && r0 + NV <= n) {
+#pragma unroll
+      for (int j = 0; j < NV; j += 4) *(float4 *)(p + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (r0 + j < n) p[j] = x[j];
+    }
+    return;
+  }
+  uint16_t *p = (uint16_t *)base + row + r0;
+  uint32_t b[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) b[j] = dtype == SIM_F16 ? f16_bits(x[j]) : bf16_bits(x[j]);
+  if (vec && r0 + NV <= n) {
+#pragma unroll
+    for (int j = 0; j < NV; j += 8)
+      *(uint4 *)(p + j) = make_uint4(b[j] | b[j + 1] << 16, b[j + 2] | b[j + 3] << 16, b[j + 4] | b[j + 5] << 16,
+                                     b[j + 6] | b[j + 7] << 16);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (r0 + j < n) p[j] = (uint16_t)b[j];
+  }
+}
+
+// ---- settings, and which scenarios a policy has ----
+
+__device__ __forceinline__ float policy_temperature(const PolicyArgs &a, int p) {
+  return a.settings ? a.settings[(int64_t)p * 4] : a.temperature;
+}
+
+struct Cut {
+  float T;
+  int k;        // at most so many
+  float p, m;   // top_p, min_p
+  bool ok;
+};
+
+__device__ __forceinline__ Cut policy_cut(const PolicyArgs &a, int p) {
+  float T = a.temperature, k = a.top_k, tp = a.top_p, mp = a.min_p;
+  if (a.settings) {
+    const float *s = a.settings + (int64_t)p * 4;
+    T = s[0], k = s[1], tp = s[2], mp = s[3];
+  }
+  Cut c;
+  c.ok = T >= 0 && T < kInf && k >= 0 && tp >= 0 && tp <= 1 && mp >= 0 && mp <= 1;
+  c.k = k >= 1 ? (int)fminf(k, (float)SIM_MAX_RES) : SIM_MAX_RES;
+  if (T == 0 || tp == 0) c.k = 1;
+  c.T = T == 0 ? 1.0f : T;
+  c.p = tp == 0 ? 1.0f : tp, c.m = mp;
+  return c;
+}
+
+__device__ __forceinline__ int policy_of(const PolicyArgs &a, int64_t s) {
+  return (int)(((a.phase + s) / a.block) % a.n_pol);
+}
+
+// f(s) for every scenario s < n_scen of policy p, in rising order.
+template <class F>
+__device__ __forceinline__ void for_scenarios(const PolicyArgs &a, int p, int64_t n_scen, F f) {
+  if (a.period == INT64_MAX && p > 0 && a.block > INT64_MAX / p) return;  // no scenario reaches it
+  int64_t t = (int64_t)p * a.block - a.phase;
+  if (t <= -a.block) t += a.period;  // at INT64_MAX, t is behind every scenario then
+  while (t < n_scen) {
+    const int64_t end = a.block < n_scen - t ? t + a.block : n_scen;
+    for (int64_t s = t > 0 ? t : 0; s < end; ++s) f(s);
+    if (a.period >= n_scen - t) break;
+    t += a.period;
+  }
+}
+
+// ---- a row's distribution ----
+
+// Larger for larger logits; 0 for -inf, equal for the two zeros.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  return x == -kInf ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+
+// Partial sums of a row's kept weights w = exp((l - max) / T), in 64 bits.
+template <int NV>
+struct RowSums {
+  double c[NV];  // up to and with this lane's resource j
+  double total;
+  int last;      // the last resource of positive weight
+  bool ok;
+};
+
+template <int G, int NV>
+__device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, int g, RowSums<NV> &out) {
+  float m = x[0];
+  int bad = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    m = fmaxf(m, x[j]);
+    bad |= x[j] != x[j];
+  }
+  m = group_max<G>(m);
+  bad = group_sum<G>(bad);
+  out.ok = !bad && cut.ok && m > -kInf && m < kInf;
+  double w[NV];
+  uint32_t key[NV], keep = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    w[j] = x[j] > -kInf ? exp(((double)x[j] - (double)m) / (double)cut.T) : 0.0;
+    key[j] = order_key(x[j]);
+    keep |= (key[j] ? 1u : 0u) << j;
+  }
+  const int n = group_sum<G>(__popc(keep));
+  uint32_t kmax = 0, kmin = 0xFFFFFFFFu;
+  if (cut.k < n || cut.p < 1) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      kmax = max(kmax, key[j]);
+      kmin = min(kmin, key[j] ? key[j] : 0xFFFFFFFFu);
+    }
+    kmax = group_umax<G>(kmax);
+    kmin = group_umin<G>(kmin);
+  }
+  const int hb = kmax > kmin ? 31 - __clz(kmax ^ kmin) : -1;    // the highest bit in which keys differ
+  const uint32_t prefix = hb < 31 ? kmax & ~((2u << hb) - 1u) : 0u;
+  const uint32_t common = hb < 0 ? kmax : prefix;
+  if (cut.k < n) {
+    // the largest tau with at least k keys >= tau, bit by bit
+    uint32_t tau = common;
+    int have = n;
+    for (int b = hb; b >= 0 && have > cut.k; --b) {
+      const uint32_t cand = tau | 1u << b;
+      int c = 0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) c += key[j] >= cand;
+      c = group_sum<G>(c);
+      if (c >= cut.k) tau = cand, have = c;
+    }
+    int ties = 0, above = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      ties += key[j] == tau;
+      above += key[j] > tau;
+    }
+    int all;
+    int rank = group_before<G>(ties, g, all);
+    // where the loop ended early, tau itself may be no key: everything at or above it is kept
+    const int room = cut.k - (have > cut.k ? group_sum<G>(above) : 0);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const bool tie = key[j] == tau;
+      const bool in = have > cut.k ? key[j] > tau || (tie && rank < room) : key[j] >= tau;
+      rank += tie;
+      if (!in) keep &= ~(1u << j);
+    }
+  }
+  if (cut.p < 1) {
+    double mass = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) mass += keep >> j & 1 ? w[j] : 0.0;
+    const double target = (double)cut.p * group_sum<G>(mass);
+    // the largest tau such that the kept keys >= tau hold the target; those
+    // from `sure` on hold less and all stay
+    uint32_t tau = common;
+    uint64_t sure = 1ull << 32;
+    double held = 0;
+    int n_tau = group_sum<G>(__popc(keep)), n_sure = 0;
+    for (int b = hb; b >= 0 && n_tau - n_sure > 1; --b) {
+      const uint32_t cand = tau | 1u << b;
+      double s = 0;
+      int c = 0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const bool in = (keep >> j & 1) && key[j] >= cand;
+        s += in ? w[j] : 0.0;
+        c += in;
+      }
+      s = group_sum<G>(s);
+      c = group_sum<G>(c);
+      if (s >= target)
+        tau = cand, n_tau = c;
+      else
+        sure = cand, n_sure = c, held = s;
+    }
+    int ties = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) ties += (keep >> j & 1) && key[j] >= tau && key[j] < sure;
+    int all;
+    int rank = group_before<G>(ties, g, all);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const bool tie = (keep >> j & 1) && key[j] >= tau && key[j] < sure;
+      const bool in = key[j] >= sure || (tie && held + rank * w[j] < target);
+      rank += tie;
+      if (!in) keep &= ~(1u << j);
+    }
+  }
+  if (cut.m > 0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (w[j] < (double)cut.m) keep &= ~(1u << j);
+  }
+  double sum = 0;
+  int last = -1;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const bool in = keep >> j & 1;
+    sum += in ? w[j] : 0.0;
+    out.c[j] = sum;
+    if (in && w[j] > 0) last = g * NV + j;
+  }
+  const double before = group_before<G>(sum, g, out.total);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) out.c[j] += before;
+  out.last = (int)group_umax<G>((uint32_t)(last + 1)) - 1;
+}
+
+// A block's tile: 2^log_pol policies (or scenarios) by the groups left.
+struct Tile {
+  int log_pol;
+  int per;  // op steps of a block
+};
+
+template <int G, int NV>
+__global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
+                                                            uint16_t *place, int64_t ld_place, Tile t) {
+  const int g = threadIdx.x % G, grp = threadIdx.x / G;
+  const int np = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
+  const int64_t pol_tiles = (a.n_pol + np - 1) / np;
+  const int64_t pol = blockIdx.x % pol_tiles * np + (grp & (np - 1));
+  const int64_t v0 = blockIdx.x / pol_tiles * (int64_t)nv * t.per + (grp >> t.log_pol);
+  if (pol >= a.n_pol) return;
+  const Cut cut = policy_cut(a, (int)pol);
+  for (int i = 0; i < t.per; ++i) {
+    const int64_t v = v0 + (int64_t)i * nv;
+    if (v >= a.n_ops) return;
+    float x[NV];
+    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
+    RowSums<NV> row;
+    row_sums<G, NV>(x, cut, g, row);
+    for_scenarios(a, (int)pol, n_scen, [&](int64_t s) {
+      const float us = u[v * ld_u + s];
+      const double target = (double)fmaxf(us, 0.0f) * row.total;
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) n += row.c[j] <= target;
+      n = min(group_sum<G>(n), row.last);
+      if (g == 0) place[v * ld_place + s] = row.ok && us == us ? (uint16_t)n : kNoPlace;
+    });
+  }
+}
+
+// A row's softmax in 32 bits: d = l - max, e = exp(d / T), their sum.
+template <int NV>
+struct RowExp {
+  float d[NV], e[NV];
+  float sum;   // NaN for an invalid row
+  bool empty;
+};
+
+template <int G, int NV>
+__device__ __forceinline__ void row_exp(const float (&x)[NV], float T, RowExp<NV> &o) {
+  float m = x[0];
+#pragma unroll
+  for (int j = 1; j < NV; ++j) m = fmaxf(m, x[j]);
+  m = group_max<G>(m);
+  float nan = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) nan = x[j] != x[j] ? x[j] : nan;  // the maximum passes over NaN
+  float s = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    o.d[j] = x[j] == -kInf ? -kInf : x[j] - m;  // inf - inf: NaN
+    o.e[j] = expf(o.d[j] / T);
+    s += o.e[j];
+  }
+  o.sum = group_sum<G>(s + nan);
+  if (!(T > 0 && T < kInf)) o.sum = __builtin_nanf("");
+  o.empty = m == -kInf && o.sum == o.sum;
+}
+
+template <int G, int NV>
+__global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t n_scen, const uint16_t *place,
+                                                          int64_t ld_place, double *part, Tile t) {
+  __shared__ double red[kThreads / G];
+  const int g = threadIdx.x % G, grp = threadIdx.x / G;
+  const int ns = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
+  const int64_t scen_tiles = (n_scen + ns - 1) / ns;
+  const int64_t s = blockIdx.x % scen_tiles * ns + (grp & (ns - 1));
+  const int64_t chunk = blockIdx.x / scen_tiles;
+  double sum = 0;
+  if (s < n_scen) {
+    const int pol = policy_of(a, s);
+    const float T = policy_temperature(a, pol);
+    for (int i = 0; i < t.per; ++i) {
+      const int64_t v = chunk * nv * t.per + (int64_t)i * nv + (grp >> t.log_pol);
+      if (v >= a.n_ops) break;
+      float x[NV];
+      load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
+      RowExp<NV> row;
+      row_exp<G, NV>(x, T, row);
+      const int at = place[v * ld_place + s];
+      float d = -kInf;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (g * NV + j == at && at < a.n_res) d = row.d[j];
+      d = group_max<G>(d);
+      sum += (double)(row.sum != row.sum ? row.sum : row.empty || d == -kInf ? -kInf : d / T - logf(row.sum));
+    }
+  }
+  if (g == 0) red[grp] = sum;
+  __syncthreads();
+  if (threadIdx.x < ns) {
+    const int64_t so = blockIdx.x % scen_tiles * ns + threadIdx.x;
+    double all = 0;
+    for (int i = 0; i < nv; ++i) all += red[(i << t.log_pol) + threadIdx.x];
+    if (so < n_scen) part[chunk * n_scen + so] = all;
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void k_policy_join(const double *part, int64_t chunks, int64_t n_scen,
+                                                          float *logp) {
+  const int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (s >= n_scen) return;
+  double sum = 0;
+  for (int64_t c = 0; c < chunks; ++c) sum += part[c * n_scen + s];
+  logp[s] = (float)sum;
+}
+
+// The gradient of a row from its softmax and what every resource received.
+template <int G, int NV>
+__device__ __forceinline__ void row_grad(const RowExp<NV> &row, float T, const float (&h)[NV], float (&out)[NV]) {
+  float w = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) w += row.d[j] == -kInf ? 0.0f : h[j];
+  w = group_sum<G>(w);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const float v = (h[j] - w * (row.e[j] / row.sum)) / T;
+    out[j] = row.sum != row.sum ? row.sum : row.d[j] == -kInf ? 0.0f : v;
+  }
+}
+
+template <int G, int NV>
+__global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t n_scen, const uint16_t *place,
+                                                          int64_t ld_place, const float *weight, PolicyOut grad, Tile t) {
+  const int g = threadIdx.x % G, grp = threadIdx.x / G;
+  const int np = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
+  const int64_t pol_tiles = (a.n_pol + np - 1) / np;
+  const int64_t pol = blockIdx.x % pol_tiles * np + (grp & (np - 1));
+  const int64_t v0 = blockIdx.x / pol_tiles * (int64_t)nv * t.per + (grp >> t.log_pol);
+  if (pol >= a.n_pol) return;
+  const float T = policy_temperature(a, (int)pol);
+  for (int i = 0; i < t.per; ++i) {
+    const int64_t v = v0 + (int64_t)i * nv;
+    if (v >= a.n_ops) return;
+    float x[NV], h[NV], out[NV];
+    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
+    RowExp<NV> row;
+    row_exp<G, NV>(x, T, row);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) h[j] = 0;
+    for_scenarios(a, (int)pol, n_scen, [&](int64_t s) {
+      const int at = place[v * ld_place + s];
+      const float w = weight[s];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) h[j] += g * NV + j == at ? w : 0.0f;
+    });
+    row_grad<G, NV>(row, T, h, out);
+    store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g * NV, a.n_res, grad.vec, out);
+  }
+}
+
+// LDS of one wavefront is read and written in order; this keeps the compiler to it.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+template <int G, int NV>
+__global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, PolicyTop top, const float *weight,
+                                                             float *loss, PolicyOut grad, int64_t rows) {
+  __shared__ float lds_q[kThreads * NV];
+  __shared__ uint32_t lds_first[kThreads * NV];
+  const int g = threadIdx.x % G, grp = threadIdx.x / G, r0 = g * NV;
+  float *q = lds_q + grp * (G * NV);
+  uint32_t *first = lds_first + grp * (G * NV);  // the entry that names a resource first
+  const int64_t n_groups = (int64_t)gridDim.x * (kThreads / G);
+  for (int64_t row_id = (int64_t)blockIdx.x * (kThreads / G) + grp; row_id < rows; row_id += n_groups) {
+    const int64_t pol = row_id / a.n_ops, v = row_id - pol * a.n_ops;
+    const float T = policy_temperature(a, (int)pol);
+    float x[NV];
+    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, a.n_res, a.vec, x);
+    RowExp<NV> row;
+    row_exp<G, NV>(x, T, row);
+    const uint16_t *ids = top.res + pol * top.ld_res_pol + v * top.ld_res_op;
+    const int64_t lrow = pol * top.ld_log_pol + v * top.ld_log_op;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) q[r0 + j] = 0, first[r0 + j] = 0xFFFFFFFFu;
+    float m = -kInf;
+    wave_order();
+    for (int k = g; k < top.top; k += G) {
+      const int id = ids[k];
+      if (id >= a.n_res) continue;
+      const float y = load_elem(top.logits, a.dtype, lrow + k);
+      m = fmaxf(m, y);
+      if (y != -kInf) atomicMin(&first[id], (uint32_t)k);
+    }
+    m = group_max<G>(m);
+    float sum = 0;
+    int again = 0, any = 0;
+    wave_order();
+    for (int k = g; k < top.top; k += G) {
+      const int id = ids[k];
+      if (id >= a.n_res) continue;
+      const float y = load_elem(top.logits, a.dtype, lrow + k);
+      if (y == -kInf) continue;
+      const float e = expf((y - m) / T);
+      sum += e;
+      any = 1;
+      if (first[id] == (uint32_t)k)
+        q[id] = e;
+      else
+        again = 1;
+    }
+    sum = group_sum<G>(sum);
+    any = group_sum<G>(any);
+    again = group_sum<G>(again);
+    wave_order();
+    if (again && g == 0)  // a resource named twice: the later entries, in order
+      for (int k = 0; k < top.top; ++k) {
+        const int id = ids[k];
+        if (id >= a.n_res) continue;
+        const float y = load_elem(top.logits, a.dtype, lrow + k);
+        if (y != -kInf && first[id] != (uint32_t)k) q[id] += expf((y - m) / T);
+      }
+    wave_order();
+    float l = 0, out[NV];
+    const float ls = logf(row.sum);
+    const float wt = weight ? weight[row_id] : 1.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const float qj = any ? q[r0 + j] / sum : 0.0f;
+      if (qj > 0) l += qj * (logf(qj) - (row.d[j] / T - ls));
+      const float pi = row.e[j] / row.sum;
+      const float v1 = wt * (pi - qj) / T;
+      out[j] = row.d[j] == -kInf || !any ? 0.0f : v1;
+    }
+    l = group_sum<G>(l);
+    const float nan = row.sum + (any ? sum : 0.0f);
+    if (row.empty && any) l = kInf;
+    if (nan != nan) l = nan;
+    if (g == 0) loss[row_id] = l;
+    if (grad.p) {
+      if (nan != nan) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) out[j] = nan;
+      }
+      store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, grad.vec, out);
+    }
+    wave_order();
+  }
+}
+
+// ---- launches ----
+
+// f(G, NV) as compile-time constants: the smallest group of lanes, at eight
+// resources a lane, that holds a row (sixteen a lane beyond 512).
+template <class F>
+int by_row(int n_res, F f) {
+#define MLSIM_ROW(G, NV) f(std::integral_constant<int, G>{}, std::integral_constant<int, NV>{})
+  if (n_res <= 8) return MLSIM_ROW(1, 8);
+  if (n_res <= 16) return MLSIM_ROW(2, 8);
+  if (n_res <= 32) return MLSIM_ROW(4, 8);
+  if (n_res <= 64) return MLSIM_ROW(8, 8);
+  if (n_res <= 128) return MLSIM_ROW(16, 8);
+  if (n_res <= 256) return MLSIM_ROW(32, 8);
+  if (n_res <= 512) return MLSIM_ROW(64, 8);
+  return MLSIM_ROW(64, 16);
+#undef MLSIM_ROW
+}
+
+int row_lanes(int n_res) {
+  int g = 1;
+  while (g < 64 && g * 8 < n_res) g *= 2;
+  return g;
+}
+
+int log2_at_least(int64_t n, int most) {
+  int l = 0;
+  while ((1 << l) < most && ((int64_t)1 << l) < n) ++l;
+  return l;
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? SIM_OK : SIM_E_HIP; }
+
+constexpr int64_t kMaxBlocks = INT32_MAX;
+
+// Row kernels: up to 32 policies side by side (so that the scenarios of
+// neighbouring policies are written together), the other groups along the ops.
+int row_tile(const PolicyArgs &a, Tile &t, int64_t &blocks) {
+  const int ng = kThreads / row_lanes(a.n_res);
+  t.log_pol = log2_at_least(a.n_pol, std::min(32, ng));
+  const int64_t np = 1 << t.log_pol, nv = ng >> t.log_pol, pol_tiles = (a.n_pol + np - 1) / np;
+  t.per = (int)std::max<int64_t>(1, std::min<int64_t>(16, pol_tiles * ((a.n_ops + nv - 1) / nv) / 2048));
+  blocks = pol_tiles * ((a.n_ops + nv * t.per - 1) / (nv * t.per));
+  return blocks > kMaxBlocks ? SIM_E_LIMIT : SIM_OK;
+}
+
+int64_t logp_tile(const PolicyArgs &a, int64_t n_scen, Tile &t, int64_t &blocks) {
+  const int ng = kThreads / row_lanes(a.n_res);
+  t.log_pol = log2_at_least(n_scen, std::min(32, ng));
+  const int64_t ns = 1 << t.log_pol, nv = ng >> t.log_pol, tiles = (n_scen + ns - 1) / ns;
+  const int64_t steps = (a.n_ops + nv - 1) / nv;
+  t.per = (int)std::min<int64_t>(steps, std::max<int64_t>(4, steps * tiles / 4096));
+  const int64_t chunks = (steps + t.per - 1) / t.per;
+  blocks = tiles * chunks;
+  return chunks;
+}
+
+}  // namespace
+
+int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, int64_t ld_u, uint16_t *place,
+                         int64_t ld_place, hipStream_t st) {
+  Tile t;
+  int64_t blocks;
+  if (int rc = row_tile(a, t, blocks)) return rc;
+  return by_row(a.n_res, [&](auto G, auto NV) {
+    k_policy_sample<G(), NV()><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, t);
+    return launched();
+  });
+}
+
+int64_t policy_work(const PolicyArgs &a, int64_t n_scen) {
+  Tile t;
+  int64_t blocks;
+  return logp_tile(a, n_scen, t, blocks) * n_scen * 8;
+}
+
+int launch_policy_logp(const PolicyArgs &a, int64_t n_scen, const uint16_t *place, int64_t ld_place, float *logp,
+                       void *work, hipStream_t st) {
+  Tile t;
+  int64_t blocks;
+  const int64_t chunks = logp_tile(a, n_scen, t, blocks);
+  if (blocks > kMaxBlocks) return SIM_E_LIMIT;
+  int rc = by_row(a.n_res, [&](auto G, auto NV) {
+    k_policy_logp<G(), NV()><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, (double *)work, t);
+    return launched();
+  });
+  if (rc) return rc;
+  k_policy_join<<<dim3((unsigned)((n_scen + kThreads - 1) / kThreads)), dim3(kThreads), 0, st>>>((const double *)work, chunks, n_scen, logp);
+  return launched();
+}
+
+int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *place, int64_t ld_place,
+                       const float *weight, const PolicyOut &grad, void *, hipStream_t st) {
+  Tile t;
+  int64_t blocks;
+  if (int rc = row_tile(a, t, blocks)) return rc;
+  return by_row(a.n_res, [&](auto G, auto NV) {
+    k_policy_grad<G(), NV()><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t);
+    return launched();
+  });
+}
+
+int launch_policy_distill(const PolicyArgs &a, const PolicyTop &top, const float *weight, float *loss,
+                          const PolicyOut &grad, hipStream_t st) {
+  const int64_t rows = (int64_t)a.n_pol * a.n_ops;
+  return by_row(a.n_res, [&](auto G, auto NV) {
+    const int64_t per = kThreads / G(), blocks = std::min<int64_t>((rows + per - 1) / per, 16384);
+    k_policy_distill<G(), NV()><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, top, weight, loss, grad, rows);
+    return launched();
+  });
+}
+
+}  // namespace mlsim

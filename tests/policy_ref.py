@@ -1,0 +1,186 @@
+"""Plain 64-bit numpy forms of the placement policy operators, one row at a
+time, with the error bounds that the GPU tests hold the kernels to.
+
+EPS is half a step of float32: every float32 operation is off by at most EPS
+relative to its result, the exponential and the logarithm by a few of them."""
+import numpy as np
+
+EPS = 2.0**-24
+#: half a step of the type that a gradient is rounded to
+HALF_STEP = {"float32": 2.0**-24, "bfloat16": 2.0**-8, "float16": 2.0**-11}
+#: below this a float16 is spaced evenly: half its step there
+HALF_TINY = {"float32": 0.0, "bfloat16": 0.0, "float16": 2.0**-25}
+NO_PLACE = 65535
+
+
+def policy_of(s, block, scen0, n_pol):
+    return ((scen0 + s) // block) % n_pol
+
+
+def settings_of(n_pol, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """float64 [n_pol, 4], each value as float32 holds it."""
+    cols = [np.broadcast_to(np.asarray(x, np.float32), (n_pol,)) for x in (temperature, top_k, top_p, min_p)]
+    return np.stack(cols, 1).astype(np.float64)
+
+
+def kept_sums(x, T, k, p, m):
+    """(C, last) of one row: the sums of the kept weights and the last resource
+    of positive weight; None where it has no valid distribution."""
+    if np.isnan(x).any() or (x == np.inf).any() or (x == -np.inf).all():
+        return None
+    if not (0 <= T < np.inf and k >= 0 and 0 <= p <= 1 and 0 <= m <= 1):
+        return None
+    order = np.lexsort((np.arange(x.size), -x))
+    order = order[x[order] > -np.inf]
+    if T == 0 or p == 0:
+        k = 1
+    w = np.exp((x - x.max()) / (T if T else 1.0))
+    order = order[:int(k)] if k >= 1 else order
+    ws = w[order]
+    if 0 < p < 1:
+        before = np.concatenate([[0.0], np.cumsum(ws)[:-1]])
+        order = order[(before < p * ws.sum()) | (np.arange(order.size) == 0)]
+        ws = w[order]
+    order = order[(ws >= m) | (np.arange(order.size) == 0)]
+    kept = np.zeros(x.size)
+    kept[order] = w[order]
+    return np.cumsum(kept), np.flatnonzero(kept)[-1]
+
+
+def draw(C, last, u):
+    place = np.searchsorted(C, np.maximum(u, 0.0) * C[-1], side="right")
+    return np.where(np.isnan(u), NO_PLACE, np.minimum(place, last))
+
+
+def sample(logits, u, settings, block=1, scen0=0):
+    P, N, R = logits.shape
+    S = u.shape[1]
+    pol = policy_of(np.arange(S), block, scen0, P)
+    place = np.full((N, S), NO_PLACE, np.int64)
+    for p in np.unique(pol):
+        at = np.flatnonzero(pol == p)
+        for v in range(N):
+            sums = kept_sums(logits[p, v], *settings[p])
+            if sums is not None:
+                place[v, at] = draw(*sums, u[v, at])
+    return place
+
+
+def log_pi(x, T):
+    """(log-probabilities, z) of one row; NaN where it is invalid, -inf where empty."""
+    if np.isnan(x).any() or (x == np.inf).any() or not 0 < T < np.inf:
+        return np.full(x.size, np.nan), np.zeros(x.size)
+    if (x == -np.inf).all():
+        return np.full(x.size, -np.inf), np.zeros(x.size)
+    z = (x - x.max()) / T
+    return z - np.log(np.exp(z).sum()), np.where(np.isfinite(z), z, 0.0)
+
+
+def logp(logits, place, settings, block=1, scen0=0):
+    """(logp [S], bound [S]).  A term's z = (l - max) / T carries three
+    roundings, its logarithm of the sum those of at most 1024 exponentials added
+    by lane and then across lanes: EPS (4 |z| + 40).  At most 32 terms are added
+    in 32 bits (EPS * 32 of their magnitudes), the rest in 64, and the total is
+    rounded once."""
+    P, N, R = logits.shape
+    S = place.shape[1]
+    pol = policy_of(np.arange(S), block, scen0, P)
+    total, size, off = np.zeros(S), np.zeros(S), np.zeros(S)
+    for p in np.unique(pol):
+        at = np.flatnonzero(pol == p)
+        for v in range(N):
+            lp, z = log_pi(logits[p, v], settings[p, 0])
+            a = place[v, at]
+            ok = a < R
+            t = np.where(ok, lp[np.minimum(a, R - 1)], np.nan if np.isnan(lp).any() else -np.inf)
+            total[at] += t
+            size[at] += np.where(np.isfinite(t), np.abs(t), 0)
+            off[at] += 4 * np.abs(z[np.minimum(a, R - 1)]) + 40
+    return total, EPS * (33 * size + off)
+
+
+def grad(logits, place, weight, settings, block=1, scen0=0, dtype="float32"):
+    """(grad [P, N, R], bound).  A resource's sum h of n weights is off by at
+    most EPS n sum |w|; W adds at most 30 roundings of sum |h|; pi as in logp."""
+    P, N, R = logits.shape
+    S = place.shape[1]
+    pol = policy_of(np.arange(S), block, scen0, P)
+    g, tol = np.zeros((P, N, R)), np.zeros((P, N, R))
+    for p in range(P):
+        at = np.flatnonzero(pol == p)
+        T = settings[p, 0]
+        for v in range(N):
+            lp, z = log_pi(logits[p, v], T)
+            if np.isnan(lp).any():
+                g[p, v] = np.nan
+                continue
+            allowed = logits[p, v] > -np.inf
+            a, w = place[v, at], weight[at]
+            ok = a < R
+            h = np.bincount(a[ok], w[ok], R)[:R] * allowed
+            n = np.bincount(a[ok], minlength=R)[:R] * allowed
+            A = np.bincount(a[ok], np.abs(w[ok]), R)[:R] * allowed
+            W = h.sum()
+            pi = np.exp(lp)
+            g[p, v] = np.where(allowed, (h - W * pi) / T, 0)
+            d_w = EPS * ((n * A).sum() + 30 * np.abs(h).sum())
+            d = EPS * n * A + pi * d_w + np.abs(W) * pi * EPS * (4 * np.abs(z) + 44)
+            d = (d + EPS * 2 * (np.abs(h) + np.abs(W) * pi)) / T + 4 * EPS * np.abs(g[p, v])
+            tol[p, v] = d + HALF_STEP[dtype] * (np.abs(g[p, v]) + d) + HALF_TINY[dtype]
+    return g, tol
+
+
+def distill(logits, ids, top, settings, weight=None, dtype="float32"):
+    """(loss [P, N], its bound, grad, its bound)."""
+    P, N, R = logits.shape
+    K = ids.shape[2]
+    loss, ltol = np.zeros((P, N)), np.zeros((P, N))
+    g, gtol = np.zeros((P, N, R)), np.zeros((P, N, R))
+    for p in range(P):
+        T = settings[p, 0]
+        for v in range(N):
+            lp, z = log_pi(logits[p, v], T)
+            allowed = logits[p, v] > -np.inf
+            use = (ids[p, v] < R) & (top[p, v] != -np.inf)
+            y = top[p, v][use]
+            if np.isnan(lp).any() or np.isnan(y).any() or (y == np.inf).any():
+                loss[p, v] = np.nan
+                g[p, v] = np.nan
+                continue
+            if not use.any():
+                continue
+            y = (y - y.max()) / T
+            t = np.exp(y) / np.exp(y).sum()
+            i = ids[p, v][use]
+            q = np.bincount(i, t, R)[:R]
+            # an entry's weight: the roundings of y, of the exponential, of a sum of K and of the quotient
+            dq = np.bincount(i, t * EPS * (4 * np.abs(y) + K + 40), R)[:R]
+            pi = np.exp(lp)
+            dpi = pi * EPS * (4 * np.abs(z) + 44)
+            pos = q > 0
+            if (pos & ~allowed).any():
+                loss[p, v] = np.inf
+            else:
+                term = np.zeros(R)
+                term[pos] = q[pos] * (np.log(q[pos]) - lp[pos])
+                loss[p, v] = term.sum()
+                dterm = np.zeros(R)
+                lq = np.log(q[pos])
+                dterm[pos] = dq[pos] * (1 + np.abs(lq - lp[pos])) + q[pos] * EPS * (4 * np.abs(z[pos]) + 44 + 4 * np.abs(lq) + 4 * np.abs(lp[pos]))
+                ltol[p, v] = dterm.sum() + 24 * EPS * np.abs(term).sum() + EPS * abs(loss[p, v])
+            w = 1.0 if weight is None else weight[p, v]
+            g[p, v] = np.where(allowed, w * (pi - q) / T, 0)
+            d = abs(w) / T * (dpi + dq) + 4 * EPS * np.abs(g[p, v])
+            gtol[p, v] = d + HALF_STEP[dtype] * (np.abs(g[p, v]) + d) + HALF_TINY[dtype]
+    return loss, ltol, g, gtol
+
+
+def near(got, want, tol, what):
+    """Every value within its bound; infinities and NaN in the same places."""
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), f"{what}: NaN elsewhere"
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf]), f"{what}: infinities differ"
+    fine = np.isfinite(want)
+    off = np.abs(got[fine] - want[fine]) - np.broadcast_to(tol, want.shape)[fine]
+    assert not (off > 0).any() and np.isfinite(got[fine]).all(), f"{what}: {off.max():.3g} over the bound"

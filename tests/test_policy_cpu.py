@@ -1,0 +1,150 @@
+"""Placement policies on the host: refusals before any HIP call, and the plain
+forms that the GPU tests compare with, checked against each other."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2002_06790_amd as mlsim
+import policy_ref as ref
+
+FAKE = 4096  # an address that no call below gets to read
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(mlsim.LIB_PATH):
+        mlsim.build()
+    return mlsim.lib()
+
+
+def struct(**kw):
+    d = dict(logits=FAKE, ld_pol=12, ld_op=3, block=1, scen0=0, settings=None, temperature=1.0, top_k=0, top_p=1.0,
+             min_p=0.0, dtype=0, n_pol=2, n_ops=4, n_res=3)
+    d.update(kw)
+    return mlsim._PolicyStruct(**d)
+
+
+BAD = [dict(n_pol=0), dict(n_ops=-1), dict(n_res=0), dict(block=0), dict(scen0=-1), dict(dtype=3), dict(dtype=-1),
+       dict(ld_pol=-1), dict(ld_op=-3), dict(logits=None), dict(logits=FAKE + 2), dict(logits=FAKE + 1, dtype=1),
+       dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")), dict(top_k=-1),
+       dict(top_p=-0.5), dict(top_p=1.5), dict(top_p=float("nan")), dict(min_p=-0.1), dict(min_p=1.1),
+       dict(min_p=float("nan")), dict(settings=FAKE + 1), dict(scen0=2**63 - 4), dict(ld_op=2**60), dict(ld_pol=2**62)]
+
+
+@pytest.mark.parametrize("kw", BAD, ids=str)
+def test_bad_policies_are_refused(L, kw):
+    p = struct(**kw)
+    assert L.sim_policy_work(p, 8) == mlsim.SIM_E_INVAL
+    assert L.sim_policy_sample(p, 8, FAKE, 8, FAKE, 8, None) == mlsim.SIM_E_INVAL
+    assert L.sim_policy_logp(p, 8, FAKE, 8, FAKE, FAKE, 2**40, None) == mlsim.SIM_E_INVAL
+    assert L.sim_policy_grad(p, 8, FAKE, 8, FAKE, FAKE, 12, 3, FAKE, 2**40, None) == mlsim.SIM_E_INVAL
+    if kw != dict(scen0=2**63 - 4):  # has no scenarios
+        assert L.sim_policy_distill(p, FAKE, 4, 1, FAKE, 4, 1, 1, None, FAKE, None, 0, 0, None) == mlsim.SIM_E_INVAL
+
+
+def test_limits_are_refused(L):
+    assert L.sim_policy_work(struct(n_res=1025, ld_op=1025), 8) == mlsim.SIM_E_LIMIT
+    assert L.sim_policy_work(struct(n_ops=2**24 + 1), 8) == mlsim.SIM_E_LIMIT
+    assert L.sim_policy_work(struct(), 2**40 + 1) == mlsim.SIM_E_LIMIT
+    assert L.sim_policy_work(struct(), -1) == mlsim.SIM_E_INVAL
+    assert L.sim_policy_work(None, 1) == mlsim.SIM_E_INVAL
+    assert L.sim_policy_work(struct(), 8) >= 0
+
+
+def test_bad_arrays_are_refused(L):
+    p, E = struct(), mlsim.SIM_E_INVAL
+    assert L.sim_policy_sample(p, 8, None, 8, FAKE, 8, None) == E
+    assert L.sim_policy_sample(p, 8, FAKE, 8, None, 8, None) == E
+    assert L.sim_policy_sample(p, 8, FAKE, 7, FAKE, 8, None) == E
+    assert L.sim_policy_sample(p, 8, FAKE, 8, FAKE, 7, None) == E
+    assert L.sim_policy_sample(p, 8, FAKE + 2, 8, FAKE, 8, None) == E
+    assert L.sim_policy_sample(p, 8, FAKE, 8, FAKE + 1, 8, None) == E
+    need = L.sim_policy_work(p, 8)
+    for place, ld, out, work, size in ((None, 8, FAKE, FAKE, need), (FAKE, 7, FAKE, FAKE, need), (FAKE, 8, None, FAKE, need),
+                                       (FAKE, 8, FAKE + 2, FAKE, need), (FAKE + 1, 8, FAKE, FAKE, need)):
+        assert L.sim_policy_logp(p, 8, place, ld, out, work, size, None) == E
+    if need:
+        assert L.sim_policy_logp(p, 8, FAKE, 8, FAKE, FAKE, need - 1, None) == E
+        assert L.sim_policy_logp(p, 8, FAKE, 8, FAKE, None, need, None) == E
+        assert L.sim_policy_logp(p, 8, FAKE, 8, FAKE, FAKE + 4, need, None) == E
+    for place, ld, w, g in ((None, 8, FAKE, FAKE), (FAKE, 7, FAKE, FAKE), (FAKE, 8, None, FAKE), (FAKE, 8, FAKE, None),
+                            (FAKE, 8, FAKE + 1, FAKE), (FAKE, 8, FAKE, FAKE + 2)):
+        assert L.sim_policy_grad(p, 8, place, ld, w, g, 12, 3, FAKE, need, None) == E
+    for ld_pol, ld_op in ((11, 3), (12, 2), (0, 3), (12, 0), (3, 5), (-12, 3), (2**62, 3)):  # rows over one another
+        assert L.sim_policy_grad(p, 8, FAKE, 8, FAKE, FAKE, ld_pol, ld_op, FAKE, need, None) == E
+
+    def distill(res=FAKE, top=1, logits=FAKE, loss=FAKE, grad=None, ld=(4, 1, 4, 1), weight=None):
+        return L.sim_policy_distill(p, res, ld[0], ld[1], logits, ld[2], ld[3], top, weight, loss, grad, 12, 2, None)
+
+    for kw in (dict(res=None), dict(logits=None), dict(loss=None), dict(top=0), dict(top=1025), dict(ld=(-1, 1, 4, 1)),
+               dict(ld=(4, 1, 4, -1)), dict(res=FAKE + 1), dict(logits=FAKE + 2), dict(loss=FAKE + 2), dict(weight=FAKE + 2),
+               dict(grad=FAKE)):
+        assert distill(**kw) == E, kw
+
+
+def test_nothing_to_do(L):
+    p = struct()
+    assert L.sim_policy_sample(p, 0, None, 0, None, 0, None) == mlsim.SIM_OK
+    assert L.sim_policy_logp(p, 0, None, 0, None, None, 0, None) == mlsim.SIM_OK
+    none = struct(n_ops=0, logits=None)
+    assert L.sim_policy_sample(none, 5, None, 0, None, 0, None) == mlsim.SIM_OK
+    assert L.sim_policy_grad(none, 5, None, 0, None, None, 0, 0, None, 0, None) == mlsim.SIM_OK
+    assert L.sim_policy_distill(none, None, 0, 0, None, 0, 0, 1, None, None, None, 0, 0, None) == mlsim.SIM_OK
+    assert L.sim_policy_work(none, 5) == 0
+
+
+def test_struct_is_the_header_s():
+    """Field order and size as a C compiler lays out sim_policy."""
+    assert ctypes.sizeof(mlsim._PolicyStruct) == 80
+    assert mlsim._PolicyStruct.settings.offset == 40 and mlsim._PolicyStruct.n_res.offset == 76
+
+
+def test_python_refuses_host_tensors():
+    with pytest.raises(TypeError):
+        mlsim.Policy(torch.zeros(4, 3))
+    with pytest.raises(TypeError):
+        mlsim.Policy(np.zeros((4, 3)))
+
+
+def test_plain_sample_keeps_what_the_settings_say():
+    x = np.array([1.0, 3.0, 3.0, -np.inf, 2.0])
+
+    def kept(T=1.0, k=0, p=1.0, m=0.0):
+        C, _ = ref.kept_sums(x, T, k, p, m)
+        return list(np.flatnonzero(np.diff(np.concatenate([[0.0], C])) > 0))
+
+    assert kept() == [0, 1, 2, 4]
+    assert kept(k=2) == [1, 2] and kept(k=1) == [1] and kept(T=0) == [1] and kept(p=0.0) == [1]
+    assert kept(k=3) == [1, 2, 4] and kept(m=0.3) == [1, 2, 4] and kept(m=1.0) == [1, 2]
+    assert kept(p=0.1) == [1] and kept(p=0.5) == [1, 2] and kept(k=2, p=0.4) == [1]
+    for bad in (np.nan, np.inf):
+        assert ref.kept_sums(np.array([0.0, bad]), 1.0, 0, 1.0, 0.0) is None
+    assert ref.kept_sums(np.full(3, -np.inf), 1.0, 0, 1.0, 0.0) is None
+
+
+def test_plain_gradients_agree_with_differences():
+    rng = np.random.default_rng(4)
+    P, N, R, S = 2, 3, 5, 7
+    x = rng.normal(size=(P, N, R))
+    x[0, 1, 3] = -np.inf
+    st = ref.settings_of(P, [0.5, 2.0])
+    place = rng.integers(0, 3, (N, S))
+    w = rng.normal(size=S)
+    g, _ = ref.grad(x, place, w, st, block=2, scen0=3)
+    ids, top = rng.integers(0, 3, (P, N, 4)), rng.normal(size=(P, N, 4))
+    dw = rng.random((P, N))
+    _, _, dg, _ = ref.distill(x, ids, top, st, dw)
+    for p, v, r in np.ndindex(P, N, R):
+        if x[p, v, r] == -np.inf:
+            assert g[p, v, r] == 0 and dg[p, v, r] == 0
+            continue
+        up, dn = x.copy(), x.copy()
+        up[p, v, r] += 1e-5
+        dn[p, v, r] -= 1e-5
+        f = [(w * ref.logp(y, place, st, 2, 3)[0]).sum() for y in (up, dn)]
+        assert abs((f[0] - f[1]) / 2e-5 - g[p, v, r]) < 1e-7
+        f = [(dw * ref.distill(y, ids, top, st)[0]).sum() for y in (up, dn)]
+        assert abs((f[0] - f[1]) / 2e-5 - dg[p, v, r]) < 1e-7
