@@ -47,9 +47,9 @@ int make_policy(const sim_policy *p, int64_t n_scen, PolicyArgs &a) {
   a.logits = p->logits;
   a.ld_pol = p->ld_pol;
   a.ld_op = p->ld_op;
-  a.block = p->block;
-  a.period = p->block > INT64_MAX / p->n_pol ? INT64_MAX : p->block * p->n_pol;
-  a.phase = p->scen0 % a.period;  // a saturated period is beyond scen0 + n_scen
+  a.block = p->n_pol == 1 ? INT64_MAX : p->block;
+  a.period = a.block > INT64_MAX / p->n_pol ? INT64_MAX : a.block * p->n_pol;
+  a.phase = p->n_pol == 1 ? 0 : p->scen0 % a.period;  // a saturated period is beyond scen0 + n_scen
   a.settings = p->settings;
   a.temperature = p->temperature;
   a.top_k = (float)std::min(p->top_k, SIM_MAX_RES);

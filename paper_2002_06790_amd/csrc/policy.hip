@@ -374,10 +374,12 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
   }
 }
 
-// A row's softmax in 32 bits: d = l - max, e = exp(d / T), their sum.
+// A row's softmax in 32 bits: z = (l - max) / T, e = exp z, their sum.  exp z
+// is the machine's 2^(z log2 e), off by 2^-24 (2 |z| + 2) of itself beside z's
+// own roundings: below what the sum's logarithm and its ratios carry anyway.
 template <int NV>
 struct RowExp {
-  float d[NV], e[NV];
+  float z[NV], e[NV];
   float sum;   // NaN for an invalid row
   bool empty;
 };
@@ -392,10 +394,11 @@ __device__ __forceinline__ void row_exp(const float (&x)[NV], float T, RowExp<NV
 #pragma unroll
   for (int j = 0; j < NV; ++j) nan = x[j] != x[j] ? x[j] : nan;  // the maximum passes over NaN
   float s = 0;
+  const float inv = 1.0f / T;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    o.d[j] = x[j] == -kInf ? -kInf : x[j] - m;  // inf - inf: NaN
-    o.e[j] = expf(o.d[j] / T);
+    o.z[j] = x[j] == -kInf ? -kInf : (x[j] - m) * inv;  // inf - inf: NaN
+    o.e[j] = __builtin_amdgcn_exp2f(o.z[j] * 1.44269504f);
     s += o.e[j];
   }
   o.sum = group_sum<G>(s + nan);
@@ -427,9 +430,9 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t 
       float d = -kInf;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (g * NV + j == at && at < a.n_res) d = row.d[j];
+        if (g * NV + j == at && at < a.n_res) d = row.z[j];
       d = group_max<G>(d);
-      sum += (double)(row.sum != row.sum ? row.sum : row.empty || d == -kInf ? -kInf : d / T - logf(row.sum));
+      sum += (double)(row.sum != row.sum ? row.sum : row.empty || d == -kInf ? -kInf : d - logf(row.sum));
     }
   }
   if (g == 0) red[grp] = sum;
@@ -442,12 +445,152 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t 
   }
 }
 
-__global__ __launch_bounds__(kThreads) void k_policy_join(const double *part, int64_t chunks, int64_t n_scen,
-                                                          float *logp) {
-  const int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (s >= n_scen) return;
+// The smaller of two pairs of 16 bits.
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {
+  typedef unsigned short pair __attribute__((ext_vector_type(2)));
+  pair x, y;
+  __builtin_memcpy(&x, &a, 4);
+  __builtin_memcpy(&y, &b, 4);
+  x = __builtin_elementwise_min(x, y);
+  __builtin_memcpy(&a, &x, 4);
+  return a;
+}
+
+// E consecutive places from p on, two a word as memory holds them; 65535
+// behind `have`.  `whole`: every lane of the wavefront has all eight, one
+// 16-byte load at any even address.  Nothing here reads what was loaded, so
+// several loads stay in flight.
+template <int E>
+__device__ __forceinline__ void load_places(const uint16_t *p, int have, bool whole, uint32_t (&w)[(E + 1) / 2]) {
+  if (E == 8 && whole) {
+    __builtin_memcpy(w, p, sizeof(w));
+  } else {
+#pragma unroll
+    for (int i = 0; i < (E + 1) / 2; ++i) {
+      const uint32_t lo = 2 * i < have ? p[2 * i] : kNoPlace;
+      const uint32_t hi = 2 * i + 1 < have ? p[2 * i + 1] : kNoPlace;
+      w[i] = lo | hi << 16;
+    }
+  }
+}
+
+template <int N>
+__device__ __forceinline__ uint32_t place_at(const uint32_t (&w)[N], int e) {
+  return (w[e / 2] >> (16 * (e & 1))) & 0xFFFFu;
+}
+
+// A batch cut into pieces of at most `span` scenarios of one policy: piece t
+// of run j (the scenarios up to the next change of policy).
+struct Pieces {
+  int64_t first;    // scenarios of run 0 before the batch
+  int64_t runs, per_run, span;
+};
+
+struct Piece {
+  int64_t beg, end;
+  int pol;
+};
+
+__device__ __forceinline__ Piece piece_of(const PolicyArgs &a, const Pieces &ps, int64_t n_scen, int64_t i) {
+  const int64_t j = i / ps.per_run, t = i - j * ps.per_run;
+  const int64_t left = j ? a.block - ps.first : 0;  // j > 0: block is below the batch's end
+  const int64_t beg = j ? left + (j - 1) * a.block : 0;
+  const int64_t len = j ? a.block : a.block - ps.first;
+  const int64_t end = len < n_scen - beg ? beg + len : n_scen;
+  Piece p;
+  p.beg = beg + t * ps.span;
+  p.end = ps.span < end - p.beg ? p.beg + ps.span : end;
+  p.pol = (int)((a.phase / a.block + j) % a.n_pol);
+  return p;
+}
+
+// Log-probabilities where many scenarios share a row.  A block takes a piece
+// of up to E scenarios a thread and a chunk of the ops: it puts the logarithms
+// of as many rows as it has groups of lanes into LDS, then every thread adds up
+// its scenarios' entries, one 16-byte load of eight places per row.  Entry n_res stands for a
+// place that is no resource.
+template <int G, int NV, int E>
+__global__ __launch_bounds__(kThreads) void k_policy_logp_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
+                                                               int64_t ld_place, float *part, Pieces ps, int64_t n_pieces,
+                                                               int ops_per) {
+  constexpr int kRows = kThreads / G;  // rows of one table
+  constexpr int kAhead = 4;            // rows whose places are loaded together
+  __shared__ float table[kRows * (G * NV + 1)];
+  const int g = threadIdx.x % G, grp = threadIdx.x / G, R = a.n_res;
+  const int64_t chunk = blockIdx.x / n_pieces;
+  const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - chunk * n_pieces);
+  if (pc.beg >= pc.end) return;
+  const float T = policy_temperature(a, pc.pol);
+  const int64_t s0 = pc.beg + (int64_t)threadIdx.x * E;
+  const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - s0));
+  const bool whole = __all(have == E);
+  const int v_end = (int)min((int64_t)a.n_ops, (chunk + 1) * ops_per);
+  double total[E] = {};
+  for (int v0 = (int)(chunk * ops_per); v0 < v_end; v0 += kRows) {
+    const int rows = min(kRows, v_end - v0);
+    uint32_t at[kAhead][(E + 1) / 2];
+    auto load = [&](int r) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        load_places<E>(place + (int64_t)(v0 + min(r + i, rows - 1)) * ld_place + s0, have, whole, at[i]);
+    };
+    load(0);
+    if (grp < rows) {
+      float x[NV];
+      load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + (v0 + grp) * a.ld_op, g * NV, R, a.vec, x);
+      RowExp<NV> row;
+      row_exp<G, NV>(x, T, row);
+      const float ls = logf(row.sum);
+      float *t = table + grp * (R + 1);
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (g * NV + j < R) t[g * NV + j] = row.sum != row.sum ? row.sum : row.z[j] == -kInf ? -kInf : row.z[j] - ls;
+      if (g == 0) t[R] = row.sum != row.sum ? row.sum : -kInf;
+    }
+    __syncthreads();
+    float sum[E] = {};  // at most 32 terms, then 64 bits
+    for (int r = 0; r < rows; r += kAhead) {
+      uint32_t now[kAhead][(E + 1) / 2];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+        for (int e = 0; e < (E + 1) / 2; ++e) now[i][e] = min_pair(at[i][e], (uint32_t)R * 0x10001u);
+      if (r + kAhead < rows) load(r + kAhead);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (r + i >= rows) break;
+        const float *t = table + (r + i) * (R + 1);
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += t[place_at(now[i], e)];
+      }
+      if (((r + kAhead) & 31) == 0 || r + kAhead >= rows) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) total[e] += (double)sum[e], sum[e] = 0;
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (e < have) part[chunk * n_scen + s0 + e] = (float)total[e];
+}
+
+constexpr int kJoinScen = 16;
+
+// The chunks' sums joined in order: sixteen lanes a scenario.
+template <class F>
+__global__ __launch_bounds__(kThreads) void k_policy_join(const F *part, int64_t chunks, int64_t n_scen, float *logp) {
+  constexpr int kScen = kJoinScen, kLanes = kThreads / kScen;
+  __shared__ double red[kLanes][kScen];
+  const int64_t s = (int64_t)blockIdx.x * kScen + threadIdx.x % kScen;
+  const int lane = threadIdx.x / kScen;
   double sum = 0;
-  for (int64_t c = 0; c < chunks; ++c) sum += part[c * n_scen + s];
+  if (s < n_scen)
+    for (int64_t c = lane; c < chunks; c += kLanes) sum += (double)part[c * n_scen + s];
+  red[lane][threadIdx.x % kScen] = sum;
+  __syncthreads();
+  if (lane || s >= n_scen) return;
+  for (int i = 1; i < kLanes; ++i) sum += red[i][threadIdx.x];
   logp[s] = (float)sum;
 }
 
@@ -456,12 +599,12 @@ template <int G, int NV>
 __device__ __forceinline__ void row_grad(const RowExp<NV> &row, float T, const float (&h)[NV], float (&out)[NV]) {
   float w = 0;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) w += row.d[j] == -kInf ? 0.0f : h[j];
+  for (int j = 0; j < NV; ++j) w += row.z[j] == -kInf ? 0.0f : h[j];
   w = group_sum<G>(w);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const float v = (h[j] - w * (row.e[j] / row.sum)) / T;
-    out[j] = row.sum != row.sum ? row.sum : row.d[j] == -kInf ? 0.0f : v;
+    out[j] = row.sum != row.sum ? row.sum : row.z[j] == -kInf ? 0.0f : v;
   }
 }
 
@@ -565,10 +708,10 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const float qj = any ? q[r0 + j] / sum : 0.0f;
-      if (qj > 0) l += qj * (logf(qj) - (row.d[j] / T - ls));
+      if (qj > 0) l += qj * (logf(qj) - (row.z[j] - ls));
       const float pi = row.e[j] / row.sum;
       const float v1 = wt * (pi - qj) / T;
-      out[j] = row.d[j] == -kInf || !any ? 0.0f : v1;
+      out[j] = row.z[j] == -kInf || !any ? 0.0f : v1;
     }
     l = group_sum<G>(l);
     const float nan = row.sum + (any ? sum : 0.0f);
@@ -642,6 +785,45 @@ int64_t logp_tile(const PolicyArgs &a, int64_t n_scen, Tile &t, int64_t &blocks)
   return chunks;
 }
 
+// Pieces of at most `span` scenarios; runs shorter than that are one each.
+Pieces make_pieces(const PolicyArgs &a, int64_t n_scen, int64_t span) {
+  Pieces p;
+  p.span = span;
+  p.first = a.phase % a.block;
+  p.runs = a.block - p.first >= n_scen ? 1 : 1 + (n_scen - (a.block - p.first) + a.block - 1) / a.block;
+  p.per_run = (std::min(a.block, n_scen) + span - 1) / span;
+  return p;
+}
+
+// Whether scenarios share rows enough that a row's table is worth making: the
+// row kernels work through a whole row for every scenario.
+bool long_runs(const PolicyArgs &a, int64_t n_scen) { return std::min(a.block, n_scen) >= 4; }
+
+struct LogpRuns {
+  Pieces ps;
+  int64_t pieces, chunks;
+  int ops_per;
+  bool wide;  // eight scenarios a thread
+};
+
+LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
+  LogpRuns l;
+  const int rows = kThreads / row_lanes(a.n_res);
+  l.wide = std::min(a.block, n_scen) >= 8 * 64;
+  l.ps = make_pieces(a, n_scen, (int64_t)kThreads * (l.wide ? 8 : 1));
+  l.pieces = l.ps.runs * l.ps.per_run;
+  // Whole tables of rows, and at most three blocks a CU, so that all run at
+  // once: 20000 ops of 64 resources in 16384 scenarios take 117 us with 720
+  // blocks (5.6 TB/s, what a plain read reaches), 127 with 632 and 138 with 1256,
+  // which leave some CUs a block more to do than others.
+  const int64_t tables = (a.n_ops + rows - 1) / rows, most = 768;
+  const int64_t want = std::max<int64_t>(1, std::min(tables, most / std::min(l.pieces, most)));
+  const int64_t per = (tables + want - 1) / want;
+  l.ops_per = (int)(per * rows);
+  l.chunks = (tables + per - 1) / per;
+  return l;
+}
+
 }  // namespace
 
 int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, int64_t ld_u, uint16_t *place,
@@ -656,6 +838,10 @@ int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, in
 }
 
 int64_t policy_work(const PolicyArgs &a, int64_t n_scen) {
+  if (long_runs(a, n_scen)) {
+    const LogpRuns l = logp_runs(a, n_scen);
+    return l.chunks > 1 ? (l.chunks * n_scen * 4 + 7) / 8 * 8 : 0;
+  }
   Tile t;
   int64_t blocks;
   return logp_tile(a, n_scen, t, blocks) * n_scen * 8;
@@ -663,6 +849,24 @@ int64_t policy_work(const PolicyArgs &a, int64_t n_scen) {
 
 int launch_policy_logp(const PolicyArgs &a, int64_t n_scen, const uint16_t *place, int64_t ld_place, float *logp,
                        void *work, hipStream_t st) {
+  const int64_t join = (n_scen + kJoinScen - 1) / kJoinScen;
+  if (join > kMaxBlocks) return SIM_E_LIMIT;
+  if (long_runs(a, n_scen)) {
+    const LogpRuns l = logp_runs(a, n_scen);
+    if (l.pieces * l.chunks > kMaxBlocks) return SIM_E_LIMIT;
+    float *to = l.chunks > 1 ? (float *)work : logp;
+    const dim3 grid((unsigned)(l.pieces * l.chunks));
+    const int rc = by_row(a.n_res, [&](auto G, auto NV) {
+      if (l.wide)
+        k_policy_logp_runs<G(), NV(), 8><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.pieces, l.ops_per);
+      else
+        k_policy_logp_runs<G(), NV(), 1><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.pieces, l.ops_per);
+      return launched();
+    });
+    if (rc || l.chunks == 1) return rc;
+    k_policy_join<<<dim3((unsigned)join), dim3(kThreads), 0, st>>>((const float *)work, l.chunks, n_scen, logp);
+    return launched();
+  }
   Tile t;
   int64_t blocks;
   const int64_t chunks = logp_tile(a, n_scen, t, blocks);
@@ -672,7 +876,7 @@ int launch_policy_logp(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
     return launched();
   });
   if (rc) return rc;
-  k_policy_join<<<dim3((unsigned)((n_scen + kThreads - 1) / kThreads)), dim3(kThreads), 0, st>>>((const double *)work, chunks, n_scen, logp);
+  k_policy_join<<<dim3((unsigned)join), dim3(kThreads), 0, st>>>((const double *)work, chunks, n_scen, logp);
   return launched();
 }
 
