@@ -15,34 +15,63 @@ constexpr int kThreads = 256;
 constexpr float kInf = __builtin_inff();
 constexpr uint16_t kNoPlace = 65535;
 
-// ---- values across the lanes of a group (xor partners stay inside it) ----
+// ---- values across the lanes of a group ----
+
+// The value of the lane O away within its 2 O: lanes whose O-lane blocks hold
+// equal values (the state of a reduction before step O) get the other block's.
+// Data-parallel moves up to 8, row swaps for 16 and 32: nothing goes through LDS.
+template <int O>
+__device__ __forceinline__ uint32_t partner(uint32_t v) {
+  if constexpr (O == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true);         // quad 1 0 3 2
+  else if constexpr (O == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true);    // quad 2 3 0 1
+  else if constexpr (O == 4) return __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true);   // mirrored in 8
+  else if constexpr (O == 8) return __builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, true);   // mirrored in 16
+  else if constexpr (O == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return (threadIdx.x & 16) ? r[0] : r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (threadIdx.x & 32) ? r[0] : r[1];
+  }
+}
+
+template <int O, class F>
+__device__ __forceinline__ F partner_of(F v) {
+  uint32_t w[sizeof(F) / 4];
+  __builtin_memcpy(w, &v, sizeof(F));
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(F) / 4; ++i) w[i] = partner<O>(w[i]);
+  __builtin_memcpy(&v, w, sizeof(F));
+  return v;
+}
+
+// op over the G lanes of a group, the result in all of them.
+template <int G, class F, class Op>
+__device__ __forceinline__ F group_all(F v, Op op) {
+  if constexpr (G > 1) v = op(v, partner_of<1>(v));
+  if constexpr (G > 2) v = op(v, partner_of<2>(v));
+  if constexpr (G > 4) v = op(v, partner_of<4>(v));
+  if constexpr (G > 8) v = op(v, partner_of<8>(v));
+  if constexpr (G > 16) v = op(v, partner_of<16>(v));
+  if constexpr (G > 32) v = op(v, partner_of<32>(v));
+  return v;
+}
 
 template <int G>
 __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-  for (int o = 1; o < G; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+  return group_all<G>(v, [](float a, float b) { return fmaxf(a, b); });
 }
-
 template <int G, class F>
 __device__ __forceinline__ F group_sum(F v) {
-#pragma unroll
-  for (int o = 1; o < G; o <<= 1) v += __shfl_xor(v, o);
-  return v;
+  return group_all<G>(v, [](F a, F b) { return a + b; });
 }
-
 template <int G>
 __device__ __forceinline__ uint32_t group_umax(uint32_t v) {
-#pragma unroll
-  for (int o = 1; o < G; o <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
-  return v;
+  return group_all<G>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
-
 template <int G>
 __device__ __forceinline__ uint32_t group_umin(uint32_t v) {
-#pragma unroll
-  for (int o = 1; o < G; o <<= 1) v = min(v, (uint32_t)__shfl_xor((int)v, o));
-  return v;
+  return group_all<G>(v, [](uint32_t a, uint32_t b) { return min(a, b); });
 }
 
 // Sum over the lanes before this one, and over all of them.
