@@ -88,6 +88,12 @@ __device__ __forceinline__ F group_before(F v, int g, F &all) {
   return g ? ex : F(0);
 }
 
+// LDS of one wavefront is read and written in order; this keeps the compiler to it.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // ---- rows ----
 
 __device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
@@ -121,9 +127,9 @@ __device__ __forceinline__ void load_row(const void *base, int32_t dtype, int64_
                                          float (&x)[NV]) {
   if (dtype == SIM_F32) {
     const float *p = (const float *)base + row + r0;
-    if (vec && r0 + NV <= n) {
+    if (NV % 8 == 0 && vec && r0 + NV <= n) {
 #pragma unroll
-      for (int j = 0; j < NV; j += 4) {
+      for (int j = 0; j + 3 < NV; j += 4) {
         const float4 t = *(const float4 *)(p + j);
         x[j] = t.x, x[j + 1] = t.y, x[j + 2] = t.z, x[j + 3] = t.w;
       }
@@ -135,9 +141,9 @@ __device__ __forceinline__ void load_row(const void *base, int32_t dtype, int64_
   }
   const uint16_t *p = (const uint16_t *)base + row + r0;
   const bool f16 = dtype == SIM_F16;
-  if (vec && r0 + NV <= n) {
+  if (NV % 8 == 0 && vec && r0 + NV <= n) {
 #pragma unroll
-    for (int j = 0; j < NV; j += 8) {
+    for (int j = 0; j + 7 < NV; j += 8) {
       const uint4 t = *(const uint4 *)(p + j);
       const uint32_t w[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
@@ -623,6 +629,100 @@ __global__ __launch_bounds__(kThreads) void k_policy_join(const F *part, int64_t
   logp[s] = (float)sum;
 }
 
+// ---- draws where many scenarios share a row ----
+
+// The lowest u >= 0 of float32 whose product with `total`, rounded to 64 bits,
+// is not below c: u >= border is then the same as u * total >= c.
+__device__ __forceinline__ float border(double c, double total) {
+  if (!(c > 0)) return 0;
+  const float f = (float)(c / total);
+  const float up = __uint_as_float(__float_as_uint(f) + 1);
+  if ((double)f * total < c) return up;
+  const float down = f > 0 ? __uint_as_float(__float_as_uint(f) - 1) : 0.0f;
+  return (double)down * total >= c ? down : f;
+}
+
+// E consecutive random numbers; 0 behind `have`.
+template <int E>
+__device__ __forceinline__ void load_numbers(const float *p, int have, bool whole, float (&u)[E]) {
+  if (whole) {
+    __builtin_memcpy(u, p, sizeof(u));
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) u[e] = e < have ? p[e] : 0.0f;
+  }
+}
+
+template <int E>
+__device__ __forceinline__ void store_places(uint16_t *p, int have, bool whole, const uint32_t (&at)[E]) {
+  if (whole) {
+    uint32_t w[E / 2];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) w[i] = at[2 * i] | at[2 * i + 1] << 16;
+    __builtin_memcpy(p, w, sizeof(w));
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e < have) p[e] = (uint16_t)at[e];
+  }
+}
+
+// A wavefront draws one row's placements for one piece.  The row's n_res - 1
+// borders go to LDS as float32, in the order of a binary tree's levels (node k
+// has 2k and 2k + 1 below it), so that a level's entries lie in
+// consecutive banks and a draw is log2 n_res steps k = 2k + (u >= tree[k]).
+template <int NV, int E>
+__global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, int64_t n_scen, const float *u,
+                                                                 int64_t ld_u, uint16_t *place, int64_t ld_place,
+                                                                 Pieces ps, int64_t n_pieces, int levels) {
+  constexpr int kWaves = kThreads / 64, kNodes = 64 * NV;
+  __shared__ float lds[kWaves * kNodes];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float *tree = lds + wave * kNodes;
+  const int64_t vb = blockIdx.x / n_pieces, v = vb * kWaves + wave;
+  if (v >= a.n_ops) return;
+  const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - vb * n_pieces);
+  if (pc.beg >= pc.end) return;
+  const float *pu = u + v * ld_u;
+  uint16_t *pp = place + v * ld_place;
+  bool ok;
+  {
+    float x[NV];
+    load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
+    RowSums<NV> row;
+    row_sums<64, NV>(x, policy_cut(a, pc.pol), lane, row);
+    ok = row.ok;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const uint32_t i = lane * NV + j + 1;  // border i - 1: between resources i - 1 and i
+      if (i < 1u << levels) {
+        const int z = __builtin_ctz(i);
+        tree[(1u << (levels - 1 - z)) + (i >> (z + 1))] = (int)i - 1 < row.last ? border(row.c[j], row.total) : kInf;
+      }
+    }
+  }
+  wave_order();
+  for (int64_t s = pc.beg + lane * E; s - lane * E < pc.end; s += 64 * E) {
+    const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - s));
+    const bool whole = __all(have == E);
+    float us[E];
+    load_numbers<E>(pu + s, have, whole, us);
+    uint32_t k[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      k[e] = 1;
+      us[e] = us[e] == kInf ? 2.0f : us[e];  // below the last border
+    }
+    for (int l = 0; l < levels; ++l) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) k[e] = 2 * k[e] + (fmaxf(us[e], 0.0f) >= tree[k[e]]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) k[e] = ok && us[e] == us[e] ? k[e] - (1u << levels) : kNoPlace;
+    store_places<E>(pp + s, have, whole, k);
+  }
+}
+
 // The gradient of a row from its softmax and what every resource received.
 template <int G, int NV>
 __device__ __forceinline__ void row_grad(const RowExp<NV> &row, float T, const float (&h)[NV], float (&out)[NV]) {
@@ -665,12 +765,6 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
     row_grad<G, NV>(row, T, h, out);
     store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g * NV, a.n_res, grad.vec, out);
   }
-}
-
-// LDS of one wavefront is read and written in order; this keeps the compiler to it.
-__device__ __forceinline__ void wave_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
 }
 
 template <int G, int NV>
@@ -776,6 +870,16 @@ int by_row(int n_res, F f) {
 #undef MLSIM_ROW
 }
 
+// f(NV): the resources a lane holds of a row that a wavefront has to itself.
+template <class F>
+int by_wave(int n_res, F f) {
+  if (n_res <= 64) return f(std::integral_constant<int, 1>{});
+  if (n_res <= 128) return f(std::integral_constant<int, 2>{});
+  if (n_res <= 256) return f(std::integral_constant<int, 4>{});
+  if (n_res <= 512) return f(std::integral_constant<int, 8>{});
+  return f(std::integral_constant<int, 16>{});
+}
+
 int row_lanes(int n_res) {
   int g = 1;
   while (g < 64 && g * 8 < n_res) g *= 2;
@@ -828,6 +932,8 @@ Pieces make_pieces(const PolicyArgs &a, int64_t n_scen, int64_t span) {
 // row kernels work through a whole row for every scenario.
 bool long_runs(const PolicyArgs &a, int64_t n_scen) { return std::min(a.block, n_scen) >= 4; }
 
+constexpr int64_t kLongRun = 64;  // draws of a row
+
 struct LogpRuns {
   Pieces ps;
   int64_t pieces, chunks;
@@ -857,6 +963,16 @@ LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
 
 int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, int64_t ld_u, uint16_t *place,
                          int64_t ld_place, hipStream_t st) {
+  if (std::min(a.block, n_scen) >= kLongRun) {
+    const Pieces ps = make_pieces(a, n_scen, 16384);
+    const int64_t pieces = ps.runs * ps.per_run, blocks = pieces * ((a.n_ops + 3) / 4);
+    if (blocks > kMaxBlocks) return SIM_E_LIMIT;
+    const int levels = log2_at_least(a.n_res, SIM_MAX_RES);
+    return by_wave(a.n_res, [&](auto NV) {
+      k_policy_sample_runs<NV(), 8><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, pieces, levels);
+      return launched();
+    });
+  }
   Tile t;
   int64_t blocks;
   if (int rc = row_tile(a, t, blocks)) return rc;
