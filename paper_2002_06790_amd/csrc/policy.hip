@@ -74,6 +74,15 @@ __device__ __forceinline__ uint32_t group_umin(uint32_t v) {
   return group_all<G>(v, [](uint32_t a, uint32_t b) { return min(a, b); });
 }
 
+// How many of a group's flags are set; a whole wavefront's through the scalar unit.
+template <int G, int N>
+__device__ __forceinline__ int group_count(const bool (&f)[N]) {
+  int c = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) c += G == 64 ? (int)__popcll(__ballot(f[j])) : f[j];
+  return G == 64 ? c : group_sum<G>(c);
+}
+
 // Sum over the lanes before this one, and over all of them.
 template <int G, class F>
 __device__ __forceinline__ F group_before(F v, int g, F &all) {
@@ -234,10 +243,11 @@ __device__ __forceinline__ void for_scenarios(const PolicyArgs &a, int p, int64_
 
 // ---- a row's distribution ----
 
-// Larger for larger logits; 0 for -inf, equal for the two zeros.
-__device__ __forceinline__ uint32_t order_key(float x) {
+// Larger for larger logits; 0 for -inf, equal for the two zeros.  `low`: bits
+// of float32 that the logits' type does not have.
+__device__ __forceinline__ uint32_t order_key(float x, int low) {
   const uint32_t b = __float_as_uint(x + 0.0f);
-  return x == -kInf ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+  return x == -kInf ? 0u : ((b & 0x80000000u) ? ~b : b | 0x80000000u) >> low;
 }
 
 // Partial sums of a row's kept weights w = exp((l - max) / T), in 64 bits.
@@ -250,7 +260,7 @@ struct RowSums {
 };
 
 template <int G, int NV>
-__device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, int g, RowSums<NV> &out) {
+__device__ __forceinline__ void row_sums(const float (&x)[NV], int32_t dtype, const Cut &cut, int g, RowSums<NV> &out) {
   float m = x[0];
   int bad = 0;
 #pragma unroll
@@ -261,12 +271,14 @@ __device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, i
   m = group_max<G>(m);
   bad = group_sum<G>(bad);
   out.ok = !bad && cut.ok && m > -kInf && m < kInf;
+  const double inv = 1.0 / (double)cut.T;
+  const int low = dtype == SIM_F32 ? 0 : dtype == SIM_BF16 ? 16 : 13;
   double w[NV];
   uint32_t key[NV], keep = 0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    w[j] = x[j] > -kInf ? exp(((double)x[j] - (double)m) / (double)cut.T) : 0.0;
-    key[j] = order_key(x[j]);
+    w[j] = x[j] > -kInf ? exp(((double)x[j] - (double)m) * inv) : 0.0;
+    key[j] = order_key(x[j], low);
     keep |= (key[j] ? 1u : 0u) << j;
   }
   const int n = group_sum<G>(__popc(keep));
@@ -289,10 +301,10 @@ __device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, i
     int have = n;
     for (int b = hb; b >= 0 && have > cut.k; --b) {
       const uint32_t cand = tau | 1u << b;
-      int c = 0;
+      bool in[NV];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) c += key[j] >= cand;
-      c = group_sum<G>(c);
+      for (int j = 0; j < NV; ++j) in[j] = key[j] >= cand;
+      const int c = group_count<G>(in);
       if (c >= cut.k) tau = cand, have = c;
     }
     int ties = 0, above = 0;
@@ -327,15 +339,14 @@ __device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, i
     for (int b = hb; b >= 0 && n_tau - n_sure > 1; --b) {
       const uint32_t cand = tau | 1u << b;
       double s = 0;
-      int c = 0;
+      bool in[NV];
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const bool in = (keep >> j & 1) && key[j] >= cand;
-        s += in ? w[j] : 0.0;
-        c += in;
+        in[j] = (keep >> j & 1) && key[j] >= cand;
+        s += in[j] ? w[j] : 0.0;
       }
+      const int c = group_count<G>(in);
       s = group_sum<G>(s);
-      c = group_sum<G>(c);
       if (s >= target)
         tau = cand, n_tau = c;
       else
@@ -396,7 +407,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
     RowSums<NV> row;
-    row_sums<G, NV>(x, cut, g, row);
+    row_sums<G, NV>(x, a.dtype, cut, g, row);
     for_scenarios(a, (int)pol, n_scen, [&](int64_t s) {
       const float us = u[v * ld_u + s];
       const double target = (double)fmaxf(us, 0.0f) * row.total;
@@ -517,8 +528,9 @@ __device__ __forceinline__ uint32_t place_at(const uint32_t (&w)[N], int e) {
 // A batch cut into pieces of at most `span` scenarios of one policy: piece t
 // of run j (the scenarios up to the next change of policy).
 struct Pieces {
-  int64_t first;    // scenarios of run 0 before the batch
-  int64_t runs, per_run, span;
+  int64_t first, span;     // scenarios of run 0 before the batch; most scenarios of a piece
+  uint32_t per_run, n;     // pieces of a run, of the batch
+  int32_t pol;             // policy of run 0
 };
 
 struct Piece {
@@ -526,16 +538,16 @@ struct Piece {
   int pol;
 };
 
-__device__ __forceinline__ Piece piece_of(const PolicyArgs &a, const Pieces &ps, int64_t n_scen, int64_t i) {
-  const int64_t j = i / ps.per_run, t = i - j * ps.per_run;
-  const int64_t left = j ? a.block - ps.first : 0;  // j > 0: block is below the batch's end
-  const int64_t beg = j ? left + (j - 1) * a.block : 0;
+__device__ __forceinline__ Piece piece_of(const PolicyArgs &a, const Pieces &ps, int64_t n_scen, uint32_t i) {
+  const uint32_t j = i / ps.per_run, t = i - j * ps.per_run;
+  const int64_t beg = j ? a.block - ps.first + (int64_t)(j - 1) * a.block : 0;  // j > 0: block is below the batch's end
   const int64_t len = j ? a.block : a.block - ps.first;
   const int64_t end = len < n_scen - beg ? beg + len : n_scen;
   Piece p;
   p.beg = beg + t * ps.span;
   p.end = ps.span < end - p.beg ? p.beg + ps.span : end;
-  p.pol = (int)((a.phase / a.block + j) % a.n_pol);
+  const uint32_t q = ps.pol + j % (uint32_t)a.n_pol;
+  p.pol = (int)(q >= (uint32_t)a.n_pol ? q - a.n_pol : q);
   return p;
 }
 
@@ -546,22 +558,21 @@ __device__ __forceinline__ Piece piece_of(const PolicyArgs &a, const Pieces &ps,
 // place that is no resource.
 template <int G, int NV, int E>
 __global__ __launch_bounds__(kThreads) void k_policy_logp_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
-                                                               int64_t ld_place, float *part, Pieces ps, int64_t n_pieces,
-                                                               int ops_per) {
+                                                               int64_t ld_place, float *part, Pieces ps, int ops_per) {
   constexpr int kRows = kThreads / G;  // rows of one table
   constexpr int kAhead = 4;            // rows whose places are loaded together
   __shared__ float table[kRows * (G * NV + 1)];
   const int g = threadIdx.x % G, grp = threadIdx.x / G, R = a.n_res;
-  const int64_t chunk = blockIdx.x / n_pieces;
-  const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - chunk * n_pieces);
+  const uint32_t chunk = blockIdx.x / ps.n;
+  const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - chunk * ps.n);
   if (pc.beg >= pc.end) return;
   const float T = policy_temperature(a, pc.pol);
   const int64_t s0 = pc.beg + (int64_t)threadIdx.x * E;
   const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - s0));
   const bool whole = __all(have == E);
-  const int v_end = (int)min((int64_t)a.n_ops, (chunk + 1) * ops_per);
+  const int v_end = (int)min((int64_t)a.n_ops, (chunk + 1) * (int64_t)ops_per);
   double total[E] = {};
-  for (int v0 = (int)(chunk * ops_per); v0 < v_end; v0 += kRows) {
+  for (int v0 = (int)(chunk * (int64_t)ops_per); v0 < v_end; v0 += kRows) {
     const int rows = min(kRows, v_end - v0);
     uint32_t at[kAhead][(E + 1) / 2];
     auto load = [&](int r) {
@@ -633,9 +644,9 @@ __global__ __launch_bounds__(kThreads) void k_policy_join(const F *part, int64_t
 
 // The lowest u >= 0 of float32 whose product with `total`, rounded to 64 bits,
 // is not below c: u >= border is then the same as u * total >= c.
-__device__ __forceinline__ float border(double c, double total) {
+__device__ __forceinline__ float border(double c, double total, double inv) {
   if (!(c > 0)) return 0;
-  const float f = (float)(c / total);
+  const float f = (float)(c * inv);
   const float up = __uint_as_float(__float_as_uint(f) + 1);
   if ((double)f * total < c) return up;
   const float down = f > 0 ? __uint_as_float(__float_as_uint(f) - 1) : 0.0f;
@@ -674,14 +685,15 @@ __device__ __forceinline__ void store_places(uint16_t *p, int have, bool whole, 
 template <int NV, int E>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, int64_t n_scen, const float *u,
                                                                  int64_t ld_u, uint16_t *place, int64_t ld_place,
-                                                                 Pieces ps, int64_t n_pieces, int levels) {
+                                                                 Pieces ps, int levels) {
   constexpr int kWaves = kThreads / 64, kNodes = 64 * NV;
   __shared__ float lds[kWaves * kNodes];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float *tree = lds + wave * kNodes;
-  const int64_t vb = blockIdx.x / n_pieces, v = vb * kWaves + wave;
+  const uint32_t vb = blockIdx.x / ps.n;
+  const int64_t v = (int64_t)vb * kWaves + wave;
   if (v >= a.n_ops) return;
-  const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - vb * n_pieces);
+  const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - vb * ps.n);
   if (pc.beg >= pc.end) return;
   const float *pu = u + v * ld_u;
   uint16_t *pp = place + v * ld_place;
@@ -690,14 +702,15 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
     RowSums<NV> row;
-    row_sums<64, NV>(x, policy_cut(a, pc.pol), lane, row);
+    row_sums<64, NV>(x, a.dtype, policy_cut(a, pc.pol), lane, row);
     ok = row.ok;
+    const double inv = 1.0 / row.total;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const uint32_t i = lane * NV + j + 1;  // border i - 1: between resources i - 1 and i
       if (i < 1u << levels) {
         const int z = __builtin_ctz(i);
-        tree[(1u << (levels - 1 - z)) + (i >> (z + 1))] = (int)i - 1 < row.last ? border(row.c[j], row.total) : kInf;
+        tree[(1u << (levels - 1 - z)) + (i >> (z + 1))] = (int)i - 1 < row.last ? border(row.c[j], row.total, inv) : kInf;
       }
     }
   }
@@ -918,14 +931,17 @@ int64_t logp_tile(const PolicyArgs &a, int64_t n_scen, Tile &t, int64_t &blocks)
   return chunks;
 }
 
-// Pieces of at most `span` scenarios; runs shorter than that are one each.
-Pieces make_pieces(const PolicyArgs &a, int64_t n_scen, int64_t span) {
-  Pieces p;
+// Their number; a launch checks that it fits.
+int64_t make_pieces(const PolicyArgs &a, int64_t n_scen, int64_t span, Pieces &p) {
   p.span = span;
   p.first = a.phase % a.block;
-  p.runs = a.block - p.first >= n_scen ? 1 : 1 + (n_scen - (a.block - p.first) + a.block - 1) / a.block;
-  p.per_run = (std::min(a.block, n_scen) + span - 1) / span;
-  return p;
+  p.pol = (int32_t)(a.phase / a.block);
+  const int64_t left = a.block - p.first;
+  const int64_t runs = left >= n_scen ? 1 : 1 + (n_scen - left + a.block - 1) / a.block;
+  const int64_t per_run = (std::min(a.block, n_scen) + span - 1) / span;
+  p.per_run = (uint32_t)std::min(per_run, kMaxBlocks);
+  p.n = (uint32_t)std::min(runs * per_run, kMaxBlocks);
+  return runs * per_run;
 }
 
 // Whether scenarios share rows enough that a row's table is worth making: the
@@ -945,8 +961,7 @@ LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
   LogpRuns l;
   const int rows = kThreads / row_lanes(a.n_res);
   l.wide = std::min(a.block, n_scen) >= 8 * 64;
-  l.ps = make_pieces(a, n_scen, (int64_t)kThreads * (l.wide ? 8 : 1));
-  l.pieces = l.ps.runs * l.ps.per_run;
+  l.pieces = make_pieces(a, n_scen, (int64_t)kThreads * (l.wide ? 8 : 1), l.ps);
   // Whole tables of rows, and at most three blocks a CU, so that all run at
   // once: 20000 ops of 64 resources in 16384 scenarios take 117 us with 720
   // blocks (5.6 TB/s, what a plain read reaches), 127 with 632 and 138 with 1256,
@@ -964,12 +979,12 @@ LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
 int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, int64_t ld_u, uint16_t *place,
                          int64_t ld_place, hipStream_t st) {
   if (std::min(a.block, n_scen) >= kLongRun) {
-    const Pieces ps = make_pieces(a, n_scen, 16384);
-    const int64_t pieces = ps.runs * ps.per_run, blocks = pieces * ((a.n_ops + 3) / 4);
+    Pieces ps;
+    const int64_t pieces = make_pieces(a, n_scen, 4096, ps), blocks = pieces * ((a.n_ops + 3) / 4);
     if (blocks > kMaxBlocks) return SIM_E_LIMIT;
     const int levels = log2_at_least(a.n_res, SIM_MAX_RES);
     return by_wave(a.n_res, [&](auto NV) {
-      k_policy_sample_runs<NV(), 8><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, pieces, levels);
+      k_policy_sample_runs<NV(), 8><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, levels);
       return launched();
     });
   }
@@ -1003,9 +1018,9 @@ int launch_policy_logp(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
     const dim3 grid((unsigned)(l.pieces * l.chunks));
     const int rc = by_row(a.n_res, [&](auto G, auto NV) {
       if (l.wide)
-        k_policy_logp_runs<G(), NV(), 8><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.pieces, l.ops_per);
+        k_policy_logp_runs<G(), NV(), 8><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.ops_per);
       else
-        k_policy_logp_runs<G(), NV(), 1><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.pieces, l.ops_per);
+        k_policy_logp_runs<G(), NV(), 1><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.ops_per);
       return launched();
     });
     if (rc || l.chunks == 1) return rc;
