@@ -667,10 +667,11 @@ __device__ __forceinline__ void load_numbers(const float *p, int have, bool whol
 template <int E>
 __device__ __forceinline__ void store_places(uint16_t *p, int have, bool whole, const uint32_t (&at)[E]) {
   if (whole) {
-    uint32_t w[E / 2];
+    typedef uint32_t words __attribute__((ext_vector_type(E / 2), aligned(2)));
+    words w;
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) w[i] = at[2 * i] | at[2 * i + 1] << 16;
-    __builtin_memcpy(p, w, sizeof(w));
+    __builtin_nontemporal_store(w, (words *)p);
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e)
@@ -678,32 +679,45 @@ __device__ __forceinline__ void store_places(uint16_t *p, int have, bool whole, 
   }
 }
 
-// A wavefront draws one row's placements for one piece.  The row's n_res - 1
+// k = 2 k + (u >= t).  The compiler makes four instructions of this; a compare
+// whose result is the carry of an addition makes two.
+__device__ __forceinline__ void descend(uint32_t &k, float u, float t) {
+  asm("v_cmp_ge_f32 vcc, %1, %2\n\tv_addc_co_u32 %0, vcc, %0, %0, vcc" : "+v"(k) : "v"(u), "v"(t) : "vcc");
+}
+
+// WR wavefronts draw one row's placements for one piece.  The row's n_res - 1
 // borders go to LDS as float32, in the order of a binary tree's levels (node k
-// has 2k and 2k + 1 below it), so that a level's entries lie in
-// consecutive banks and a draw is log2 n_res steps k = 2k + (u >= tree[k]).
-template <int NV, int E>
+// has 2k and 2k + 1 below it), so that a level's entries lie in consecutive
+// banks and a draw is log2 n_res steps k = 2k + (u >= tree[k]), three vector
+// instructions and one LDS read each.
+template <int NV, int WR>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, int64_t n_scen, const float *u,
                                                                  int64_t ld_u, uint16_t *place, int64_t ld_place,
                                                                  Pieces ps, int levels) {
-  constexpr int kWaves = kThreads / 64, kNodes = 64 * NV;
-  __shared__ float lds[kWaves * kNodes];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float *tree = lds + wave * kNodes;
+  constexpr int E = 8, kRows = kThreads / 64 / WR, kNodes = 64 * NV;  // E: consecutive scenarios of a lane
+  __shared__ float lds[kRows * kNodes];
+  __shared__ int lds_ok[kRows];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, of_row = wave % WR;
+  float *tree = lds + wave / WR * kNodes;
   const uint32_t vb = blockIdx.x / ps.n;
-  const int64_t v = (int64_t)vb * kWaves + wave;
-  if (v >= a.n_ops) return;
+  const int64_t v = (int64_t)vb * kRows + wave / WR;
+  if (v >= a.n_ops) return;  // with WR > 1 a block has one row
   const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - vb * ps.n);
   if (pc.beg >= pc.end) return;
   const float *pu = u + v * ld_u;
   uint16_t *pp = place + v * ld_place;
-  bool ok;
-  {
+  int64_t s = pc.beg + (of_row * 64 + lane) * E;
+  float us[E];
+  auto load = [&] {
+    const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - s));
+    load_numbers<E>(pu + s, have, __all(have == E), us);
+  };
+  load();
+  if (of_row == 0) {
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
     RowSums<NV> row;
     row_sums<64, NV>(x, a.dtype, policy_cut(a, pc.pol), lane, row);
-    ok = row.ok;
     const double inv = 1.0 / row.total;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -713,26 +727,42 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
         tree[(1u << (levels - 1 - z)) + (i >> (z + 1))] = (int)i - 1 < row.last ? border(row.c[j], row.total, inv) : kInf;
       }
     }
+    if (lane == 0) lds_ok[wave / WR] = row.ok;
   }
-  wave_order();
-  for (int64_t s = pc.beg + lane * E; s - lane * E < pc.end; s += 64 * E) {
-    const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - s));
-    const bool whole = __all(have == E);
-    float us[E];
-    load_numbers<E>(pu + s, have, whole, us);
+  if (WR > 1)
+    __syncthreads();
+  else
+    wave_order();
+  const bool ok = lds_ok[wave / WR];
+  while (s - lane * E < pc.end) {
     uint32_t k[E];
+    bool nan = !ok;
+    float at[E], keep[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
+      if (e & 1) nan |= __builtin_isunordered(us[e - 1], us[e]);
+      keep[e] = us[e];
+      at[e] = __builtin_amdgcn_fmed3f(us[e], 0.0f, 2.0f);  // above 1 all are the same
       k[e] = 1;
-      us[e] = us[e] == kInf ? 2.0f : us[e];  // below the last border
     }
+    const int64_t now = s;
+    s += WR * 64 * E;
+    load();
     for (int l = 0; l < levels; ++l) {
+      float t[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) k[e] = 2 * k[e] + (fmaxf(us[e], 0.0f) >= tree[k[e]]);
+      for (int e = 0; e < E; ++e) t[e] = tree[k[e]];
+#pragma unroll
+      for (int e = 0; e < E; ++e) descend(k[e], at[e], t[e]);
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) k[e] = ok && us[e] == us[e] ? k[e] - (1u << levels) : kNoPlace;
-    store_places<E>(pp + s, have, whole, k);
+    for (int e = 0; e < E; ++e) k[e] -= 1u << levels;
+    if (__any(nan)) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) k[e] = ok && keep[e] == keep[e] ? k[e] : kNoPlace;
+    }
+    const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - now));
+    store_places<E>(pp + now, have, __all(have == E), k);
   }
 }
 
@@ -980,11 +1010,16 @@ int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, in
                          int64_t ld_place, hipStream_t st) {
   if (std::min(a.block, n_scen) >= kLongRun) {
     Pieces ps;
-    const int64_t pieces = make_pieces(a, n_scen, 4096, ps), blocks = pieces * ((a.n_ops + 3) / 4);
+    const bool cut = a.settings || a.top_k >= 1 || a.top_p < 1 || a.min_p > 0;
+    const int wr = !cut && std::min(a.block, n_scen) >= 2048 ? 4 : 1;
+    const int64_t pieces = make_pieces(a, n_scen, wr > 1 ? 8192 : 4096, ps), blocks = pieces * ((a.n_ops * (int64_t)wr + 3) / 4);
     if (blocks > kMaxBlocks) return SIM_E_LIMIT;
     const int levels = log2_at_least(a.n_res, SIM_MAX_RES);
     return by_wave(a.n_res, [&](auto NV) {
-      k_policy_sample_runs<NV(), 8><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, levels);
+      if (wr == 4)
+        k_policy_sample_runs<NV(), 4><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, levels);
+      else
+        k_policy_sample_runs<NV(), 1><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, levels);
       return launched();
     });
   }
