@@ -169,9 +169,9 @@ __device__ __forceinline__ void store_row(void *base, int32_t dtype, int64_t row
                                           const float (&x)[NV]) {
   if (dtype == SIM_F32) {
     float *p = (float *)base + row + r0;
-    if (vec && r0 + NV <= n) {
+    if (NV % 8 == 0 && vec && r0 + NV <= n) {
 #pragma unroll
-      for (int j = 0; j < NV; j += 4) *(float4 *)(p + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+      for (int j = 0; j + 3 < NV; j += 4) *(float4 *)(p + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
     } else {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
@@ -183,9 +183,9 @@ __device__ __forceinline__ void store_row(void *base, int32_t dtype, int64_t row
   uint32_t b[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) b[j] = dtype == SIM_F16 ? f16_bits(x[j]) : bf16_bits(x[j]);
-  if (vec && r0 + NV <= n) {
+  if (NV % 8 == 0 && vec && r0 + NV <= n) {
 #pragma unroll
-    for (int j = 0; j < NV; j += 8)
+    for (int j = 0; j + 7 < NV; j += 8)
       *(uint4 *)(p + j) = make_uint4(b[j] | b[j + 1] << 16, b[j + 2] | b[j + 3] << 16, b[j + 4] | b[j + 5] << 16,
                                      b[j + 6] | b[j + 7] << 16);
   } else {
@@ -227,16 +227,19 @@ __device__ __forceinline__ int policy_of(const PolicyArgs &a, int64_t s) {
   return (int)(((a.phase + s) / a.block) % a.n_pol);
 }
 
-// f(s) for every scenario s < n_scen of policy p, in rising order.
+// f(beg, end) for every run of scenarios of policy p within [from, to), in rising order.
 template <class F>
-__device__ __forceinline__ void for_scenarios(const PolicyArgs &a, int p, int64_t n_scen, F f) {
+__device__ __forceinline__ void for_runs(const PolicyArgs &a, int p, int64_t from, int64_t to, F f) {
   if (a.period == INT64_MAX && p > 0 && a.block > INT64_MAX / p) return;  // no scenario reaches it
   int64_t t = (int64_t)p * a.block - a.phase;
-  if (t <= -a.block) t += a.period;  // at INT64_MAX, t is behind every scenario then
-  while (t < n_scen) {
-    const int64_t end = a.block < n_scen - t ? t + a.block : n_scen;
-    for (int64_t s = t > 0 ? t : 0; s < end; ++s) f(s);
-    if (a.period >= n_scen - t) break;
+  if (from > t) {
+    t += (from - t) / a.period * a.period;
+    if (t <= from - a.block) t += a.period;  // at INT64_MAX, t is behind every scenario then
+  }
+  while (t < to) {
+    const int64_t beg = max(t, from), end = a.block < to - t ? t + a.block : to;
+    f(beg, end);
+    if (a.period >= to - t) break;
     t += a.period;
   }
 }
@@ -408,7 +411,8 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
     load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
     RowSums<NV> row;
     row_sums<G, NV>(x, a.dtype, cut, g, row);
-    for_scenarios(a, (int)pol, n_scen, [&](int64_t s) {
+    for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
+     for (int64_t s = beg; s < end; ++s) {
       const float us = u[v * ld_u + s];
       const double target = (double)fmaxf(us, 0.0f) * row.total;
       int n = 0;
@@ -416,6 +420,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
       for (int j = 0; j < NV; ++j) n += row.c[j] <= target;
       n = min(group_sum<G>(n), row.last);
       if (g == 0) place[v * ld_place + s] = row.ok && us == us ? (uint16_t)n : kNoPlace;
+     }
     });
   }
 }
@@ -799,15 +804,134 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
     row_exp<G, NV>(x, T, row);
 #pragma unroll
     for (int j = 0; j < NV; ++j) h[j] = 0;
-    for_scenarios(a, (int)pol, n_scen, [&](int64_t s) {
+    for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
+     for (int64_t s = beg; s < end; ++s) {
       const int at = place[v * ld_place + s];
       const float w = weight[s];
 #pragma unroll
       for (int j = 0; j < NV; ++j) h[j] += g * NV + j == at ? w : 0.0f;
+     }
     });
     row_grad<G, NV>(row, T, h, out);
     store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g * NV, a.n_res, grad.vec, out);
   }
+}
+
+// The gradient where many scenarios share a row.  A wavefront adds one row's
+// weights up by resource in a table of LDS with C = 64 / NV columns: lane i
+// adds to column i mod C, C lanes an instruction, so no two lanes of one
+// instruction meet and every entry gets its weights in one order.  (One column
+// for all would serialise the lanes of a settled policy, which choose alike.)
+// Then every lane adds up its resources' columns.  Row n_res of the table takes
+// places that are no resource.  With several splits of the batch a row's sums
+// go to `part`, and the next kernel joins them.
+template <int NV>
+__global__ __launch_bounds__(64) void k_policy_grad_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
+                                                         int64_t ld_place, const float *weight, PolicyOut grad,
+                                                         float *part, uint32_t splits, int64_t per_split) {
+  constexpr int C = 64 / NV, E = 8;
+  extern __shared__ float table[];
+  const int lane = threadIdx.x, R = a.n_res;
+  const uint32_t row_id = blockIdx.x / splits, k = blockIdx.x - row_id * splits;
+  const uint32_t pol = row_id / (uint32_t)a.n_ops, v = row_id - pol * (uint32_t)a.n_ops;
+  for (int i = lane; i < (R + 1) * C; i += 64) table[i] = 0;
+  wave_order();
+  const uint16_t *pp = place + (int64_t)v * ld_place;
+  const int64_t from = k * per_split, to = min(n_scen, from + per_split);
+  float *mine = table + lane % C;
+  auto add = [&](uint32_t at, float w) {
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+      if (NV == 1 || lane / C == q) __hip_atomic_fetch_add(mine + at * C, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+  };
+  if (a.block >= 64 * E) {
+    for_runs(a, (int)pol, from, to, [&](int64_t beg, int64_t end) {
+      int64_t s = beg + lane * E;
+      uint32_t w[E / 2];
+      float x[E];
+      auto load = [&] {
+        const int have = (int)max((int64_t)0, min((int64_t)E, end - s));
+        const bool whole = __all(have == E);
+        load_places<E>(pp + s, have, whole, w);
+        load_numbers<E>(weight + s, have, whole, x);
+      };
+      load();
+      while (s - lane * E < end) {
+        uint32_t now[E / 2];
+        float y[E];
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) now[i] = min_pair(w[i], (uint32_t)R * 0x10001u);
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = x[e];
+        s += 64 * E;
+        load();
+#pragma unroll
+        for (int e = 0; e < E; ++e) add(place_at(now, e), y[e]);
+      }
+    });
+  } else {
+    // short runs: the policy's scenarios one after another over the lanes; run
+    // j begins at t + j * period
+    const uint32_t block = (uint32_t)a.block, step_j = 64 / block, step_o = 64 - step_j * block;
+    int64_t t = (int64_t)pol * a.block - a.phase;
+    if (from > t) t += (from - t) / a.period * a.period;
+    t += lane / block * a.period;
+    uint32_t o = lane % block;
+    while (t < to) {
+      const int64_t s = t + o;
+      if (s >= from && s < to) add(min((uint32_t)pp[s], (uint32_t)R), weight[s]);
+      t += step_j * a.period;
+      o += step_o;
+      if (o >= block) o -= block, t += a.period;
+    }
+  }
+  wave_order();
+  const int r0 = lane * NV;
+  float h[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    h[j] = 0;
+    if (r0 + j < R)
+      for (int c = 0; c < C; ++c) h[j] += table[(r0 + j) * C + (lane + c) % C];  // lanes in different banks
+  }
+  if (splits > 1) {
+    float *to_part = part + ((int64_t)k * (gridDim.x / splits) + row_id) * R;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (r0 + j < R) to_part[r0 + j] = h[j];
+    return;
+  }
+  const float T = policy_temperature(a, (int)pol);
+  float x[NV], out[NV];
+  load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, R, a.vec, x);
+  RowExp<NV> row;
+  row_exp<64, NV>(x, T, row);
+  row_grad<64, NV>(row, T, h, out);
+  store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, R, grad.vec, out);
+}
+
+// The splits' sums of every row joined in order, and its gradient.
+template <int G, int NV>
+__global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, const float *part, uint32_t splits,
+                                                               uint32_t rows, PolicyOut grad) {
+  const int g = threadIdx.x % G, r0 = g * NV;
+  const uint32_t row_id = blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  if (row_id >= rows) return;
+  const uint32_t pol = row_id / (uint32_t)a.n_ops, v = row_id - pol * (uint32_t)a.n_ops;
+  const float T = policy_temperature(a, (int)pol);
+  float x[NV], h[NV], out[NV];
+  load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, a.n_res, a.vec, x);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) h[j] = 0;
+  for (uint32_t k = 0; k < splits; ++k) {
+    const float *p = part + ((int64_t)k * rows + row_id) * a.n_res + r0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) h[j] += r0 + j < a.n_res ? p[j] : 0.0f;
+  }
+  RowExp<NV> row;
+  row_exp<G, NV>(x, T, row);
+  row_grad<G, NV>(row, T, h, out);
+  store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, grad.vec, out);
 }
 
 template <int G, int NV>
@@ -1004,6 +1128,20 @@ LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
   return l;
 }
 
+struct GradRuns {
+  int64_t rows, splits, per_split;
+};
+
+// Enough wavefronts to fill the chip, none with fewer than 4096 scenarios of the batch.
+GradRuns grad_runs(const PolicyArgs &a, int64_t n_scen) {
+  GradRuns r;
+  r.rows = (int64_t)a.n_pol * a.n_ops;
+  r.splits = std::max<int64_t>(1, std::min(2048 / std::min<int64_t>(r.rows, 2048), n_scen / 4096));
+  r.per_split = ((n_scen + r.splits - 1) / r.splits + 511) / 512 * 512;
+  r.splits = (n_scen + r.per_split - 1) / r.per_split;
+  return r;
+}
+
 }  // namespace
 
 int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, int64_t ld_u, uint16_t *place,
@@ -1033,13 +1171,20 @@ int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, in
 }
 
 int64_t policy_work(const PolicyArgs &a, int64_t n_scen) {
+  int64_t logp, grad = 0;
   if (long_runs(a, n_scen)) {
     const LogpRuns l = logp_runs(a, n_scen);
-    return l.chunks > 1 ? (l.chunks * n_scen * 4 + 7) / 8 * 8 : 0;
+    logp = l.chunks > 1 ? l.chunks * n_scen * 4 : 0;
+  } else {
+    Tile t;
+    int64_t blocks;
+    logp = logp_tile(a, n_scen, t, blocks) * n_scen * 8;
   }
-  Tile t;
-  int64_t blocks;
-  return logp_tile(a, n_scen, t, blocks) * n_scen * 8;
+  if (n_scen / a.n_pol >= kLongRun) {
+    const GradRuns r = grad_runs(a, n_scen);
+    if (r.splits > 1) grad = r.splits * r.rows * a.n_res * 4;
+  }
+  return (std::max(logp, grad) + 7) / 8 * 8;
 }
 
 int launch_policy_logp(const PolicyArgs &a, int64_t n_scen, const uint16_t *place, int64_t ld_place, float *logp,
@@ -1076,7 +1221,23 @@ int launch_policy_logp(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
 }
 
 int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *place, int64_t ld_place,
-                       const float *weight, const PolicyOut &grad, void *, hipStream_t st) {
+                       const float *weight, const PolicyOut &grad, void *work, hipStream_t st) {
+  if (n_scen / a.n_pol >= kLongRun) {
+    const GradRuns r = grad_runs(a, n_scen);
+    if (r.rows * r.splits > kMaxBlocks) return SIM_E_LIMIT;
+    const uint32_t splits = (uint32_t)r.splits;
+    const dim3 grid((unsigned)(r.rows * r.splits));
+    int rc = by_wave(a.n_res, [&](auto NV) {
+      k_policy_grad_runs<NV()><<<grid, dim3(64), (size_t)(a.n_res + 1) * (64 / NV()) * 4, st>>>(a, n_scen, place, ld_place, weight, grad, (float *)work, splits, r.per_split);
+      return launched();
+    });
+    if (rc || splits == 1) return rc;
+    return by_row(a.n_res, [&](auto G, auto NV) {
+      const unsigned per = kThreads / G(), rows = (unsigned)r.rows;
+      k_policy_grad_join<G(), NV()><<<dim3((rows + per - 1) / per), dim3(kThreads), 0, st>>>(a, (const float *)work, splits, rows, grad);
+      return launched();
+    });
+  }
   Tile t;
   int64_t blocks;
   if (int rc = row_tile(a, t, blocks)) return rc;
