@@ -817,56 +817,69 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
   }
 }
 
+// Columns of a row's table below: 33 KB of LDS a wavefront, 64 KB beyond 256 resources.
+constexpr int grad_columns(int nv) { return nv <= 2 ? 32 : nv <= 8 ? 16 : 8; }
+
 // The gradient where many scenarios share a row.  A wavefront adds one row's
-// weights up by resource in a table of LDS with C = 64 / NV columns: lane i
+// weights up by resource in a table of LDS with C columns, in 64 bits: lane i
 // adds to column i mod C, C lanes an instruction, so no two lanes of one
 // instruction meet and every entry gets its weights in one order.  (One column
-// for all would serialise the lanes of a settled policy, which choose alike.)
-// Then every lane adds up its resources' columns.  Row n_res of the table takes
-// places that are no resource.  With several splits of the batch a row's sums
-// go to `part`, and the next kernel joins them.
+// for all would make the order the machine's.  An LDS addition of float64 takes
+// 9 clocks for a wavefront, one of float32 takes 193: 3 a lane.)  Then every
+// lane adds up its resources' columns.  With several splits of the batch a
+// row's sums go to `part`, and the next kernel joins them.
 template <int NV>
 __global__ __launch_bounds__(64) void k_policy_grad_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
                                                          int64_t ld_place, const float *weight, PolicyOut grad,
                                                          float *part, uint32_t splits, int64_t per_split) {
-  constexpr int C = 64 / NV, E = 8;
-  extern __shared__ float table[];
+  constexpr int C = grad_columns(NV), E = 8, kAhead = 4;  // kAhead: loads of eight places in flight
+  extern __shared__ double table[];
   const int lane = threadIdx.x, R = a.n_res;
   const uint32_t row_id = blockIdx.x / splits, k = blockIdx.x - row_id * splits;
   const uint32_t pol = row_id / (uint32_t)a.n_ops, v = row_id - pol * (uint32_t)a.n_ops;
-  for (int i = lane; i < (R + 1) * C; i += 64) table[i] = 0;
+  for (int i = lane; i < R * C; i += 64) table[i] = 0;
   wave_order();
   const uint16_t *pp = place + (int64_t)v * ld_place;
   const int64_t from = k * per_split, to = min(n_scen, from + per_split);
-  float *mine = table + lane % C;
+  double *mine = table + lane % C;
   auto add = [&](uint32_t at, float w) {
 #pragma unroll
-    for (int q = 0; q < NV; ++q)
-      if (NV == 1 || lane / C == q) __hip_atomic_fetch_add(mine + at * C, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    for (int q = 0; q < 64 / C; ++q)
+      if (lane / C == q && at < (uint32_t)R)
+        __hip_atomic_fetch_add(mine + at * C, (double)w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
   };
   if (a.block >= 64 * E) {
     for_runs(a, (int)pol, from, to, [&](int64_t beg, int64_t end) {
       int64_t s = beg + lane * E;
-      uint32_t w[E / 2];
-      float x[E];
+      uint32_t w[kAhead][E / 2];
+      float x[kAhead][E];
       auto load = [&] {
-        const int have = (int)max((int64_t)0, min((int64_t)E, end - s));
-        const bool whole = __all(have == E);
-        load_places<E>(pp + s, have, whole, w);
-        load_numbers<E>(weight + s, have, whole, x);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int64_t si = s + i * 64 * E;
+          const int have = (int)max((int64_t)0, min((int64_t)E, end - si));
+          const bool whole = __all(have == E);
+          load_places<E>(pp + si, have, whole, w[i]);
+          load_numbers<E>(weight + si, have, whole, x[i]);
+        }
       };
       load();
       while (s - lane * E < end) {
-        uint32_t now[E / 2];
-        float y[E];
+        uint32_t now[kAhead][E / 2];
+        float y[kAhead][E];
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) now[i] = min_pair(w[i], (uint32_t)R * 0x10001u);
+        for (int i = 0; i < kAhead; ++i) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = x[e];
-        s += 64 * E;
+          for (int e = 0; e < E / 2; ++e) now[i][e] = w[i][e];
+#pragma unroll
+          for (int e = 0; e < E; ++e) y[i][e] = x[i][e];
+        }
+        s += kAhead * 64 * E;
         load();
 #pragma unroll
-        for (int e = 0; e < E; ++e) add(place_at(now, e), y[e]);
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+          for (int e = 0; e < E; ++e) add(place_at(now[i], e), y[i][e]);
       }
     });
   } else {
@@ -879,7 +892,7 @@ __global__ __launch_bounds__(64) void k_policy_grad_runs(PolicyArgs a, int64_t n
     uint32_t o = lane % block;
     while (t < to) {
       const int64_t s = t + o;
-      if (s >= from && s < to) add(min((uint32_t)pp[s], (uint32_t)R), weight[s]);
+      if (s >= from && s < to) add(pp[s], weight[s]);
       t += step_j * a.period;
       o += step_o;
       if (o >= block) o -= block, t += a.period;
@@ -890,9 +903,10 @@ __global__ __launch_bounds__(64) void k_policy_grad_runs(PolicyArgs a, int64_t n
   float h[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    h[j] = 0;
+    double sum = 0;
     if (r0 + j < R)
-      for (int c = 0; c < C; ++c) h[j] += table[(r0 + j) * C + (lane + c) % C];  // lanes in different banks
+      for (int c = 0; c < C; ++c) sum += table[(r0 + j) * C + (lane + c) % C];  // lanes in different banks
+    h[j] = (float)sum;
   }
   if (splits > 1) {
     float *to_part = part + ((int64_t)k * (gridDim.x / splits) + row_id) * R;
@@ -1228,7 +1242,7 @@ int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
     const uint32_t splits = (uint32_t)r.splits;
     const dim3 grid((unsigned)(r.rows * r.splits));
     int rc = by_wave(a.n_res, [&](auto NV) {
-      k_policy_grad_runs<NV()><<<grid, dim3(64), (size_t)(a.n_res + 1) * (64 / NV()) * 4, st>>>(a, n_scen, place, ld_place, weight, grad, (float *)work, splits, r.per_split);
+      k_policy_grad_runs<NV()><<<grid, dim3(64), (size_t)a.n_res * grad_columns(NV()) * 8, st>>>(a, n_scen, place, ld_place, weight, grad, (float *)work, splits, r.per_split);
       return launched();
     });
     if (rc || splits == 1) return rc;
