@@ -507,6 +507,11 @@ __device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {
   return a;
 }
 
+// The larger.
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+  return ~min_pair(~a, ~b);
+}
+
 // E consecutive places from p on, two a word as memory holds them; 65535
 // behind `have`.  `whole`: every lane of the wavefront has all eight, one
 // 16-byte load at any even address.  Nothing here reads what was loaded, so
@@ -817,107 +822,170 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
   }
 }
 
-// Columns of a row's table below: 33 KB of LDS a wavefront, 64 KB beyond 256 resources.
-constexpr int grad_columns(int nv) { return nv <= 2 ? 32 : nv <= 8 ? 16 : 8; }
+// The largest magnitude of the weights of each block's share (NaN counts as
+// infinite), for the grid below.
+constexpr int kPeakBlocks = 64;
+__global__ __launch_bounds__(kThreads) void k_policy_peak(const float *weight, int64_t n, float *peak) {
+  __shared__ float red[kThreads / 64];
+  float m = 0;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+    const float w = fabsf(weight[i]);
+    m = w == w ? fmaxf(m, w) : kInf;
+  }
+  m = group_max<64>(m);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) peak[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
 
-// The gradient where many scenarios share a row.  A wavefront adds one row's
-// weights up by resource in a table of LDS with C columns, in 64 bits: lane i
-// adds to column i mod C, C lanes an instruction, so no two lanes of one
-// instruction meet and every entry gets its weights in one order.  (One column
-// for all would make the order the machine's.  An LDS addition of float64 takes
-// 9 clocks for a wavefront, one of float32 takes 193: 3 a lane.)  Then every
-// lane adds up its resources' columns.  With several splits of the batch a
+// A block of the kernel below has four wavefronts.  Together (WR = 4) they take
+// `rows` ops of a policy at once, so that a weight is loaded and rounded once for
+// several rows, with `columns` columns for a row's table: at most 32 KB of LDS in
+// all.  Alone (WR = 1) each takes a row of its own.
+template <int NV, int WR>
+struct GradShape {
+  static constexpr int kGroups = 4 / WR;  // of wavefronts in a block
+  static constexpr int kRows = WR == 1 || NV > 2 ? 1 : 4 / NV;
+  static constexpr int kColumns = WR == 1 ? 16 / NV : NV <= 4 ? 16 : 64 / NV;
+  static size_t lds(int n_res) { return (size_t)n_res * kGroups * kRows * kColumns * 8; }
+};
+
+// The gradient where many scenarios share a row.  Weights are added up by
+// resource in a table of LDS of float64 for every row.  A weight is first
+// rounded to a grid 2^53 / per_split times finer than a power of two above the
+// largest one (at 16384 scenarios 2^-38 of it): on that grid every sum is exact,
+// so that the lanes' order does not matter and any of them may add to any
+// entry.  Columns keep down how many meet in one.  (An LDS addition of float64
+// takes 9 clocks for a wavefront with 16 columns or more, 17 with 8, 20 with 4;
+// one of float32 takes 193, 3 a lane.)  Then a wavefront adds up a row's
+// columns and goes on to its gradient.  With several splits of the batch a
 // row's sums go to `part`, and the next kernel joins them.
-template <int NV>
-__global__ __launch_bounds__(64) void k_policy_grad_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
-                                                         int64_t ld_place, const float *weight, PolicyOut grad,
-                                                         float *part, uint32_t splits, int64_t per_split) {
-  constexpr int C = grad_columns(NV), E = 8, kAhead = 4;  // kAhead: loads of eight places in flight
-  extern __shared__ double table[];
-  const int lane = threadIdx.x, R = a.n_res;
-  const uint32_t row_id = blockIdx.x / splits, k = blockIdx.x - row_id * splits;
-  const uint32_t pol = row_id / (uint32_t)a.n_ops, v = row_id - pol * (uint32_t)a.n_ops;
-  for (int i = lane; i < R * C; i += 64) table[i] = 0;
-  wave_order();
-  const uint16_t *pp = place + (int64_t)v * ld_place;
+template <int NV, int WR>
+__global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
+                                                               int64_t ld_place, const float *weight, const float *peak,
+                                                               PolicyOut grad, double *part, uint32_t tiles,
+                                                               uint32_t splits, int64_t per_split) {
+  using S = GradShape<NV, WR>;
+  constexpr int C = S::kColumns, RB = S::kRows, E = 8;
+  extern __shared__ double lds_table[];
+  const int R = a.n_res, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int t = threadIdx.x % (64 * WR);  // of the group's lanes
+  const uint32_t id = blockIdx.x * S::kGroups + wave / WR;
+  const uint32_t tile = id / splits, k = id - tile * splits;
+  if (tile >= tiles) return;  // with WR = 4 a block is one group
+  const uint32_t per_pol = ((uint32_t)a.n_ops + RB - 1) / RB, pol = tile / per_pol, v0 = (tile - pol * per_pol) * RB;
+  const int rows = min(RB, a.n_ops - (int)v0);
+  double *table = lds_table + wave / WR * (RB * R * C);
+  // a wavefront's row once the sums are there
+  const int own = wave % WR;
+  const uint32_t v = v0 + own;
+  const bool finish = own < rows;
+  float x[NV];
+  if (finish && splits == 1)
+    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, lane * NV, R, a.vec, x);
+  for (int i = t; i < RB * R * C; i += 64 * WR) table[i] = 0;
+  const float top = group_max<64>(peak[lane]);
+  // adding and taking away 1.5 2^52 grid steps rounds to the grid
+  const double magic = top > 0 && top < kInf ? ldexp(1.5, ilogbf(top) + 64 - __clzll(per_split)) : 0.0;
+  if (WR > 1)
+    __syncthreads();
+  else
+    wave_order();
+  const uint16_t *pp = place + (int64_t)v0 * ld_place;
   const int64_t from = k * per_split, to = min(n_scen, from + per_split);
   double *mine = table + lane % C;
-  auto add = [&](uint32_t at, float w) {
-#pragma unroll
-    for (int q = 0; q < 64 / C; ++q)
-      if (lane / C == q && at < (uint32_t)R)
-        __hip_atomic_fetch_add(mine + at * C, (double)w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+  auto add = [&](int row, uint32_t at, double w) {
+    __hip_atomic_fetch_add(mine + (row * R + at) * C, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   };
   if (a.block >= 64 * E) {
     for_runs(a, (int)pol, from, to, [&](int64_t beg, int64_t end) {
-      int64_t s = beg + lane * E;
-      uint32_t w[kAhead][E / 2];
-      float x[kAhead][E];
+      int64_t s = beg + t * E;
+      uint32_t w[RB][E / 2];
+      float y[E];
       auto load = [&] {
+        const int have = (int)max((int64_t)0, min((int64_t)E, end - s));
+        const bool whole = __all(have == E);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          const int64_t si = s + i * 64 * E;
-          const int have = (int)max((int64_t)0, min((int64_t)E, end - si));
-          const bool whole = __all(have == E);
-          load_places<E>(pp + si, have, whole, w[i]);
-          load_numbers<E>(weight + si, have, whole, x[i]);
-        }
+        for (int i = 0; i < RB; ++i) load_places<E>(pp + min(i, rows - 1) * ld_place + s, have, whole, w[i]);
+        load_numbers<E>(weight + s, have, whole, y);
       };
       load();
-      while (s - lane * E < end) {
-        uint32_t now[kAhead][E / 2];
-        float y[kAhead][E];
+      while (s - t * E < end) {
+        uint32_t at[RB][E / 2];
+        double z[E];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int e = 0; e < E; ++e) z[e] = (double)y[e] + magic - magic;
 #pragma unroll
-          for (int e = 0; e < E / 2; ++e) now[i][e] = w[i][e];
+        for (int i = 0; i < RB; ++i)
 #pragma unroll
-          for (int e = 0; e < E; ++e) y[i][e] = x[i][e];
-        }
-        s += kAhead * 64 * E;
+          for (int e = 0; e < E / 2; ++e) at[i][e] = w[i][e];
+        s += 64 * WR * E;
         load();
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
+        for (int i = 0; i < RB; ++i) {
+          if (i >= rows) break;
+          uint32_t most = at[i][0];
 #pragma unroll
-          for (int e = 0; e < E; ++e) add(place_at(now[i], e), y[i][e]);
+          for (int e = 1; e < E / 2; ++e) most = max_pair(most, at[i][e]);
+          if (__any(max(most & 0xFFFFu, most >> 16) >= (uint32_t)R)) {  // no resource, or behind the end
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+              if (place_at(at[i], e) < (uint32_t)R) add(i, place_at(at[i], e), z[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) add(i, place_at(at[i], e), z[e]);
+          }
+        }
       }
     });
   } else {
     // short runs: the policy's scenarios one after another over the lanes; run
-    // j begins at t + j * period
-    const uint32_t block = (uint32_t)a.block, step_j = 64 / block, step_o = 64 - step_j * block;
-    int64_t t = (int64_t)pol * a.block - a.phase;
-    if (from > t) t += (from - t) / a.period * a.period;
-    t += lane / block * a.period;
-    uint32_t o = lane % block;
-    while (t < to) {
-      const int64_t s = t + o;
-      if (s >= from && s < to) add(pp[s], weight[s]);
-      t += step_j * a.period;
+    // j begins at b + j * period
+    const uint32_t block = (uint32_t)a.block, step_j = 64 * WR / block, step_o = 64 * WR - step_j * block;
+    int64_t b = (int64_t)pol * a.block - a.phase;
+    if (from > b) b += (from - b) / a.period * a.period;
+    b += t / block * a.period;
+    uint32_t o = t % block;
+    while (b < to) {
+      const int64_t s = b + o;
+      if (s >= from && s < to) {
+        const double z = (double)weight[s] + magic - magic;
+        for (int i = 0; i < rows; ++i) {
+          const uint32_t at = pp[i * ld_place + s];
+          if (at < (uint32_t)R) add(i, at, z);
+        }
+      }
+      b += step_j * a.period;
       o += step_o;
-      if (o >= block) o -= block, t += a.period;
+      if (o >= block) o -= block, b += a.period;
     }
   }
-  wave_order();
+  if (WR > 1)
+    __syncthreads();
+  else
+    wave_order();
+  if (!finish) return;
   const int r0 = lane * NV;
+  double sum[NV];
   float h[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    double sum = 0;
-    if (r0 + j < R)
-      for (int c = 0; c < C; ++c) sum += table[(r0 + j) * C + (lane + c) % C];  // lanes in different banks
-    h[j] = (float)sum;
+    sum[j] = 0;
+    if (r0 + j < R) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) sum[j] += table[(own * R + r0 + j) * C + (lane + c) % C];  // lanes in different banks
+    }
+    h[j] = (float)sum[j];
   }
   if (splits > 1) {
-    float *to_part = part + ((int64_t)k * (gridDim.x / splits) + row_id) * R;
+    double *to_part = part + (((int64_t)k * a.n_pol + pol) * a.n_ops + v) * R;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-      if (r0 + j < R) to_part[r0 + j] = h[j];
+      if (r0 + j < R) to_part[r0 + j] = sum[j];
     return;
   }
   const float T = policy_temperature(a, (int)pol);
-  float x[NV], out[NV];
-  load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, R, a.vec, x);
+  float out[NV];
   RowExp<NV> row;
   row_exp<64, NV>(x, T, row);
   row_grad<64, NV>(row, T, h, out);
@@ -926,7 +994,7 @@ __global__ __launch_bounds__(64) void k_policy_grad_runs(PolicyArgs a, int64_t n
 
 // The splits' sums of every row joined in order, and its gradient.
 template <int G, int NV>
-__global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, const float *part, uint32_t splits,
+__global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, const double *part, uint32_t splits,
                                                                uint32_t rows, PolicyOut grad) {
   const int g = threadIdx.x % G, r0 = g * NV;
   const uint32_t row_id = blockIdx.x * (kThreads / G) + threadIdx.x / G;
@@ -935,13 +1003,14 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, con
   const float T = policy_temperature(a, (int)pol);
   float x[NV], h[NV], out[NV];
   load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, a.n_res, a.vec, x);
-#pragma unroll
-  for (int j = 0; j < NV; ++j) h[j] = 0;
+  double sum[NV] = {};
   for (uint32_t k = 0; k < splits; ++k) {
-    const float *p = part + ((int64_t)k * rows + row_id) * a.n_res + r0;
+    const double *p = part + ((int64_t)k * rows + row_id) * a.n_res + r0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) h[j] += r0 + j < a.n_res ? p[j] : 0.0f;
+    for (int j = 0; j < NV; ++j) sum[j] += r0 + j < a.n_res ? p[j] : 0.0;
   }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) h[j] = (float)sum[j];
   RowExp<NV> row;
   row_exp<G, NV>(x, T, row);
   row_grad<G, NV>(row, T, h, out);
@@ -1144,13 +1213,19 @@ LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
 
 struct GradRuns {
   int64_t rows, splits, per_split;
+  int waves;  // of a row
 };
 
-// Enough wavefronts to fill the chip, none with fewer than 4096 scenarios of the batch.
+// Enough wavefronts to fill the chip, none with fewer than 2048 scenarios of
+// the batch; no split above 2^22, so that the weights' grid is at least 2^31
+// times finer than the largest.
 GradRuns grad_runs(const PolicyArgs &a, int64_t n_scen) {
   GradRuns r;
   r.rows = (int64_t)a.n_pol * a.n_ops;
-  r.splits = std::max<int64_t>(1, std::min(2048 / std::min<int64_t>(r.rows, 2048), n_scen / 4096));
+  r.waves = n_scen / a.n_pol >= 2048 ? 4 : 1;
+  const int64_t fill = 4096 / std::min<int64_t>(r.rows * r.waves, 4096);
+  r.splits = std::max<int64_t>(1, std::min(fill, n_scen / (r.waves * 2048)));
+  r.splits = std::max(r.splits, (n_scen + (1 << 22) - 1) >> 22);
   r.per_split = ((n_scen + r.splits - 1) / r.splits + 511) / 512 * 512;
   r.splits = (n_scen + r.per_split - 1) / r.per_split;
   return r;
@@ -1196,7 +1271,7 @@ int64_t policy_work(const PolicyArgs &a, int64_t n_scen) {
   }
   if (n_scen / a.n_pol >= kLongRun) {
     const GradRuns r = grad_runs(a, n_scen);
-    if (r.splits > 1) grad = r.splits * r.rows * a.n_res * 4;
+    grad = kPeakBlocks * 4 + (r.splits > 1 ? r.splits * r.rows * a.n_res * 8 : 0);
   }
   return (std::max(logp, grad) + 7) / 8 * 8;
 }
@@ -1239,16 +1314,26 @@ int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
   if (n_scen / a.n_pol >= kLongRun) {
     const GradRuns r = grad_runs(a, n_scen);
     if (r.rows * r.splits > kMaxBlocks) return SIM_E_LIMIT;
-    const uint32_t splits = (uint32_t)r.splits;
-    const dim3 grid((unsigned)(r.rows * r.splits));
-    int rc = by_wave(a.n_res, [&](auto NV) {
-      k_policy_grad_runs<NV()><<<grid, dim3(64), (size_t)a.n_res * grad_columns(NV()) * 8, st>>>(a, n_scen, place, ld_place, weight, grad, (float *)work, splits, r.per_split);
+    float *peak = (float *)work;
+    double *part = (double *)((char *)work + kPeakBlocks * 4);
+    const uint32_t rows = (uint32_t)r.rows, splits = (uint32_t)r.splits;
+    k_policy_peak<<<dim3(kPeakBlocks), dim3(kThreads), 0, st>>>(weight, n_scen, peak);
+    if (int rc = launched()) return rc;
+    auto go = [&](auto NV, auto WR) {
+      using S = GradShape<NV(), WR()>;
+      const uint32_t tiles = (uint32_t)(a.n_pol * ((a.n_ops + (int64_t)S::kRows - 1) / S::kRows));
+      const uint32_t blocks = (uint32_t)(((int64_t)tiles * splits + S::kGroups - 1) / S::kGroups);
+      k_policy_grad_runs<NV(), WR()><<<dim3(blocks), dim3(kThreads), S::lds(a.n_res), st>>>(
+          a, n_scen, place, ld_place, weight, peak, grad, part, tiles, splits, r.per_split);
       return launched();
+    };
+    int rc = by_wave(a.n_res, [&](auto NV) {
+      return r.waves == 4 ? go(NV, std::integral_constant<int, 4>{}) : go(NV, std::integral_constant<int, 1>{});
     });
     if (rc || splits == 1) return rc;
     return by_row(a.n_res, [&](auto G, auto NV) {
-      const unsigned per = kThreads / G(), rows = (unsigned)r.rows;
-      k_policy_grad_join<G(), NV()><<<dim3((rows + per - 1) / per), dim3(kThreads), 0, st>>>(a, (const float *)work, splits, rows, grad);
+      const unsigned per = kThreads / G();
+      k_policy_grad_join<G(), NV()><<<dim3((rows + per - 1) / per), dim3(kThreads), 0, st>>>(a, part, splits, rows, grad);
       return launched();
     });
   }
