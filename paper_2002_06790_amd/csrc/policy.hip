@@ -69,9 +69,16 @@ template <int G>
 __device__ __forceinline__ uint32_t group_umax(uint32_t v) {
   return group_all<G>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
-template <int G>
-__device__ __forceinline__ uint32_t group_umin(uint32_t v) {
-  return group_all<G>(v, [](uint32_t a, uint32_t b) { return min(a, b); });
+// The value of lane (lane ^ X), for the X that sorting needs.
+template <int X>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+  if constexpr (X == 1 || X == 2 || X == 7 || X == 15 || X == 16 || X == 32)
+    return partner<(X == 7 ? 4 : X == 15 ? 8 : X)>(v);
+  else if constexpr (X == 3) return __builtin_amdgcn_mov_dpp(v, 0x1B, 0xF, 0xF, true);   // quad 3 2 1 0
+  else if constexpr (X == 8) return __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true);  // 16 turned by 8
+  else if constexpr (X == 4) return lane_xor<3>(lane_xor<7>(v));
+  else if constexpr (X == 31) return lane_xor<15>(lane_xor<16>(v));
+  else return lane_xor<31>(lane_xor<32>(v));
 }
 
 // How many of a group's flags are set; a whole wavefront's through the scalar unit.
@@ -246,24 +253,81 @@ __device__ __forceinline__ void for_runs(const PolicyArgs &a, int p, int64_t fro
 
 // ---- a row's distribution ----
 
-// Larger for larger logits; 0 for -inf, equal for the two zeros.  `low`: bits
-// of float32 that the logits' type does not have.
-__device__ __forceinline__ uint32_t order_key(float x, int low) {
-  const uint32_t b = __float_as_uint(x + 0.0f);
-  return x == -kInf ? 0u : ((b & 0x80000000u) ? ~b : b | 0x80000000u) >> low;
+// One step of merging across lanes: against lane ^ X, whose elements are taken in
+// reverse order if FLIP; a lane
+// keeps the larger ones (bound = inf) or the smaller (-inf).
+template <int X, bool FLIP, int NV>
+__device__ __forceinline__ void exchange(float (&v)[NV], float bound) {
+  float q[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) q[j] = __uint_as_float(lane_xor<X>(__float_as_uint(v[FLIP ? NV - 1 - j : j])));
+#pragma unroll
+  for (int j = 0; j < NV; ++j) v[j] = __builtin_amdgcn_fmed3f(v[j], q[j], bound);
 }
 
-// Partial sums of a row's kept weights w = exp((l - max) / T), in 64 bits.
-template <int NV>
+template <int S, int NV>
+__device__ __forceinline__ void merge_lanes(float (&v)[NV], int g) {
+  exchange<S, false>(v, (g & S) ? -kInf : kInf);
+  if constexpr (S > 1) merge_lanes<S / 2>(v, g);
+}
+
+// Merge the sorted halves of 2 L lanes: the bitonic order, all steps the same way.
+template <int L, int G, int NV>
+__device__ __forceinline__ void merge_up(float (&v)[NV], int g) {
+  if constexpr (L < G) {
+    exchange<2 * L - 1, true>(v, (g & L) ? -kInf : kInf);
+    if constexpr (L > 1) merge_lanes<L / 2>(v, g);
+#pragma unroll
+    for (int s = NV / 2; s >= 1; s /= 2)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (!(j & s)) {
+          const float hi = fmaxf(v[j], v[j + s]), lo = fminf(v[j], v[j + s]);
+          v[j] = hi, v[j + s] = lo;
+        }
+    merge_up<2 * L, G>(v, g);
+  }
+}
+
+// Sort a group's G * NV values, the largest into element 0 of lane 0: the lanes'
+// own by the odd-even merge exchanges, then bitonic merges of lanes.
+template <int G, int NV>
+__device__ __forceinline__ void sort_row(float (&v)[NV], int g) {
+#pragma unroll
+  for (int p = 1; p < NV; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j + k < NV; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < NV && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            const float hi = fmaxf(v[i + j], v[i + j + k]), lo = fminf(v[i + j], v[i + j + k]);
+            v[i + j] = hi, v[i + j + k] = lo;
+          }
+  merge_up<1, G>(v, g);
+}
+
+// Partial sums of a row's kept weights w = exp((l - max) / T).  In 64 bits (F =
+// double) they are the definition; in 32 bits `unsure` says that a choice lies
+// within what the roundings can move: z carries five (its own, the reciprocal's, the
+// product with log2 e), so a weight is off by 2^-24 (5 |z| + 2) of itself and any
+// sum by the mean of that, where the mean |z| of a distribution over 1024 is at
+// most ln 1024; 22 additions and the product with u come on top: below 2^-17
+// of the whole sum, of which kMargin is twice.
+constexpr float kMargin = 0x1p-16f;
+
+template <class F, int NV>
 struct RowSums {
-  double c[NV];  // up to and with this lane's resource j
-  double total;
-  int last;      // the last resource of positive weight
-  bool ok;
+  F c[NV];  // up to and with this lane's resource j
+  F total;
+  int last;  // the last resource of positive weight
+  bool ok, unsure;
 };
 
-template <int G, int NV>
-__device__ __forceinline__ void row_sums(const float (&x)[NV], int32_t dtype, const Cut &cut, int g, RowSums<NV> &out) {
+template <class F, int G, int NV>
+__device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, int g, RowSums<F, NV> &out) {
+  constexpr bool kFast = sizeof(F) == 4;
   float m = x[0];
   int bad = 0;
 #pragma unroll
@@ -274,118 +338,94 @@ __device__ __forceinline__ void row_sums(const float (&x)[NV], int32_t dtype, co
   m = group_max<G>(m);
   bad = group_sum<G>(bad);
   out.ok = !bad && cut.ok && m > -kInf && m < kInf;
-  const double inv = 1.0 / (double)cut.T;
-  const int low = dtype == SIM_F32 ? 0 : dtype == SIM_BF16 ? 16 : 13;
-  double w[NV];
-  uint32_t key[NV], keep = 0;
+  const F inv = kFast ? F(1.44269504f * (1.0f / cut.T)) : F(1.0 / (double)cut.T);
+  int unsure = kFast && !(inv < F(1e30));
+  auto weight = [&](float l) -> F {
+    if constexpr (kFast)
+      return __builtin_amdgcn_exp2f((l - m) * inv);
+    else
+      return exp(((double)l - (double)m) * inv);
+  };
+  F w[NV];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    w[j] = x[j] > -kInf ? exp(((double)x[j] - (double)m) * inv) : 0.0;
-    key[j] = order_key(x[j], low);
-    keep |= (key[j] ? 1u : 0u) << j;
-  }
-  const int n = group_sum<G>(__popc(keep));
-  uint32_t kmax = 0, kmin = 0xFFFFFFFFu;
-  if (cut.k < n || cut.p < 1) {
+  for (int j = 0; j < NV; ++j) w[j] = x[j] > -kInf ? weight(x[j]) : F(0);
+  uint32_t keep = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      kmax = max(kmax, key[j]);
-      kmin = min(kmin, key[j] ? key[j] : 0xFFFFFFFFu);
-    }
-    kmax = group_umax<G>(kmax);
-    kmin = group_umin<G>(kmin);
-  }
-  const int hb = kmax > kmin ? 31 - __clz(kmax ^ kmin) : -1;    // the highest bit in which keys differ
-  const uint32_t prefix = hb < 31 ? kmax & ~((2u << hb) - 1u) : 0u;
-  const uint32_t common = hb < 0 ? kmax : prefix;
-  if (cut.k < n) {
-    // the largest tau with at least k keys >= tau, bit by bit
-    uint32_t tau = common;
-    int have = n;
-    for (int b = hb; b >= 0 && have > cut.k; --b) {
-      const uint32_t cand = tau | 1u << b;
-      bool in[NV];
+  for (int j = 0; j < NV; ++j) keep |= (x[j] > -kInf ? 1u : 0u) << j;
+  if (cut.k < SIM_MAX_RES || cut.p < 1) {
+    float s[NV];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) in[j] = key[j] >= cand;
-      const int c = group_count<G>(in);
-      if (c >= cut.k) tau = cand, have = c;
-    }
-    int ties = 0, above = 0;
+    for (int j = 0; j < NV; ++j) s[j] = x[j];
+    sort_row<G, NV>(s, g);
+    bool in[NV];  // a first part of the order
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      ties += key[j] == tau;
-      above += key[j] > tau;
-    }
-    int all;
-    int rank = group_before<G>(ties, g, all);
-    // where the loop ended early, tau itself may be no key: everything at or above it is kept
-    const int room = cut.k - (have > cut.k ? group_sum<G>(above) : 0);
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const bool tie = key[j] == tau;
-      const bool in = have > cut.k ? key[j] > tau || (tie && rank < room) : key[j] >= tau;
-      rank += tie;
-      if (!in) keep &= ~(1u << j);
-    }
-  }
-  if (cut.p < 1) {
-    double mass = 0;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) mass += keep >> j & 1 ? w[j] : 0.0;
-    const double target = (double)cut.p * group_sum<G>(mass);
-    // the largest tau such that the kept keys >= tau hold the target; those
-    // from `sure` on hold less and all stay
-    uint32_t tau = common;
-    uint64_t sure = 1ull << 32;
-    double held = 0;
-    int n_tau = group_sum<G>(__popc(keep)), n_sure = 0;
-    for (int b = hb; b >= 0 && n_tau - n_sure > 1; --b) {
-      const uint32_t cand = tau | 1u << b;
-      double s = 0;
-      bool in[NV];
+    for (int j = 0; j < NV; ++j) in[j] = s[j] > -kInf && g * NV + j < cut.k;
+    if (cut.p < 1) {
+      F ws[NV], mass = 0, all;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        in[j] = (keep >> j & 1) && key[j] >= cand;
-        s += in[j] ? w[j] : 0.0;
+        ws[j] = mass;
+        mass += in[j] ? weight(s[j]) : F(0);
       }
-      const int c = group_count<G>(in);
-      s = group_sum<G>(s);
-      if (s >= target)
-        tau = cand, n_tau = c;
-      else
-        sure = cand, n_sure = c, held = s;
-    }
-    int ties = 0;
+      const F before = group_before<G>(mass, g, all), target = (F)cut.p * all;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) ties += (keep >> j & 1) && key[j] >= tau && key[j] < sure;
-    int all;
-    int rank = group_before<G>(ties, g, all);
+      for (int j = 0; j < NV; ++j) {
+        const F b = ws[j] + before;
+        const bool first = g * NV + j == 0;
+        if constexpr (kFast) unsure |= in[j] && !first && fabsf(b - target) <= kMargin * all;
+        in[j] = in[j] && (b < target || first);
+      }
+    }
+    // the last logit of the kept part, and how many of its equals belong to it
+    float cutoff = kInf;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) cutoff = in[j] ? fminf(cutoff, s[j]) : cutoff;
+    cutoff = -group_max<G>(-cutoff);
+    bool eq[NV], eq_in[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const bool tie = (keep >> j & 1) && key[j] >= tau && key[j] < sure;
-      const bool in = key[j] >= sure || (tie && held + rank * w[j] < target);
-      rank += tie;
-      if (!in) keep &= ~(1u << j);
+      eq[j] = s[j] == cutoff;
+      eq_in[j] = eq[j] && in[j];
+    }
+    const int room = group_count<G>(eq_in);
+    keep = 0;
+    if (group_count<G>(eq) == room) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) keep |= (x[j] >= cutoff ? 1u : 0u) << j;
+    } else {
+      int ties = 0, all;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) ties += x[j] == cutoff;
+      int rank = group_before<G>(ties, g, all);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const bool tie = x[j] == cutoff;
+        keep |= (x[j] > cutoff || (tie && rank < room) ? 1u : 0u) << j;
+        rank += tie;
+      }
     }
   }
   if (cut.m > 0) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (w[j] < (double)cut.m) keep &= ~(1u << j);
+    for (int j = 0; j < NV; ++j) {
+      if constexpr (kFast) unsure |= (keep >> j & 1) && fabsf(w[j] - cut.m) <= 0x1p-15f * cut.m;
+      if (w[j] < (F)cut.m) keep &= ~(1u << j);
+    }
   }
-  double sum = 0;
+  F sum = 0;
   int last = -1;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const bool in = keep >> j & 1;
-    sum += in ? w[j] : 0.0;
+    sum += in ? w[j] : F(0);
     out.c[j] = sum;
     if (in && w[j] > 0) last = g * NV + j;
   }
-  const double before = group_before<G>(sum, g, out.total);
+  const F before = group_before<G>(sum, g, out.total);
 #pragma unroll
   for (int j = 0; j < NV; ++j) out.c[j] += before;
   out.last = (int)group_umax<G>((uint32_t)(last + 1)) - 1;
+  if constexpr (kFast) out.unsure = group_umax<G>((uint32_t)unsure) != 0;
 }
 
 // A block's tile: 2^log_pol policies (or scenarios) by the groups left.
@@ -409,8 +449,8 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
     if (v >= a.n_ops) return;
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
-    RowSums<NV> row;
-    row_sums<G, NV>(x, a.dtype, cut, g, row);
+    RowSums<double, NV> row;
+    row_sums<double, G, NV>(x, cut, g, row);
     for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
      for (int64_t s = beg; s < end; ++s) {
       const float us = u[v * ld_u + s];
@@ -726,8 +766,8 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
   if (of_row == 0) {
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
-    RowSums<NV> row;
-    row_sums<64, NV>(x, a.dtype, policy_cut(a, pc.pol), lane, row);
+    RowSums<double, NV> row;
+    row_sums<double, 64, NV>(x, policy_cut(a, pc.pol), lane, row);
     const double inv = 1.0 / row.total;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
