@@ -434,34 +434,109 @@ struct Tile {
   int per;  // op steps of a block
 };
 
+// The scenarios of a policy one by one.
+struct Scenarios {
+  int64_t s, end, t;  // s: n_scen when there is none left
+
+  __device__ __forceinline__ void run(const PolicyArgs &a, int64_t n_scen) {
+    s = t < n_scen ? max(t, (int64_t)0) : n_scen;
+    end = t < n_scen && a.block < n_scen - t ? t + a.block : n_scen;
+  }
+  __device__ __forceinline__ void begin(const PolicyArgs &a, int64_t pol, int64_t n_scen) {
+    t = n_scen;
+    if (!(a.period == INT64_MAX && pol > 0 && a.block > INT64_MAX / pol)) {  // else no scenario reaches it
+      t = pol * a.block - a.phase;
+      if (t <= -a.block) t += a.period;  // at INT64_MAX, t is behind every scenario then
+    }
+    run(a, n_scen);
+  }
+  __device__ __forceinline__ void next(const PolicyArgs &a, int64_t n_scen) {
+    if (++s < end || s >= n_scen) return;
+    t = a.period >= n_scen - t ? n_scen : t + a.period;
+    run(a, n_scen);
+  }
+};
+
+template <class T>
+__device__ __forceinline__ T from_lane(T v, int lane) {
+  uint32_t w[sizeof(T) / 4];
+  __builtin_memcpy(w, &v, sizeof(T));
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(T) / 4; ++i) w[i] = __builtin_amdgcn_readlane(w[i], lane);
+  __builtin_memcpy(&v, w, sizeof(T));
+  return v;
+}
+
+// One draw in 64 bits by a whole wavefront.
+template <int NV>
+__device__ __forceinline__ uint32_t draw_sure(const PolicyArgs &a, int64_t pol, int64_t v, float u) {
+  const int lane = threadIdx.x & 63;
+  float x[NV];
+  load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
+  RowSums<double, NV> row;
+  row_sums<double, 64, NV>(x, policy_cut(a, (int)pol), lane, row);
+  const double target = (double)fmaxf(u, 0.0f) * row.total;
+  bool in[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) in[j] = row.c[j] <= target;
+  return min(group_count<64>(in), row.last);
+}
+
+// Few scenarios a row: a group of lanes works a row out in 32 bits and draws
+// its scenarios one after another.  A draw that lies within the roundings of a border
+// (about one in a thousand at 64 resources) is done again in 64 bits by the
+// whole wavefront, so that every answer is the 64-bit one.
 template <int G, int NV>
 __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
                                                             uint16_t *place, int64_t ld_place, Tile t) {
+  constexpr int kWide = G * NV > 64 ? G * NV / 64 : 1;
   const int g = threadIdx.x % G, grp = threadIdx.x / G;
   const int np = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
   const int64_t pol_tiles = (a.n_pol + np - 1) / np;
-  const int64_t pol = blockIdx.x % pol_tiles * np + (grp & (np - 1));
+  const int64_t pol_at = blockIdx.x % pol_tiles * np + (grp & (np - 1));
   const int64_t v0 = blockIdx.x / pol_tiles * (int64_t)nv * t.per + (grp >> t.log_pol);
-  if (pol >= a.n_pol) return;
+  const bool live_pol = pol_at < a.n_pol;
+  const int64_t pol = live_pol ? pol_at : 0;
   const Cut cut = policy_cut(a, (int)pol);
+  Scenarios first;
+  first.begin(a, pol, n_scen);
   for (int i = 0; i < t.per; ++i) {
-    const int64_t v = v0 + (int64_t)i * nv;
-    if (v >= a.n_ops) return;
+    const bool live = live_pol && v0 + (int64_t)i * nv < a.n_ops;
+    if (!__any(live)) return;
+    const int64_t v = live ? v0 + (int64_t)i * nv : 0;
+    Scenarios it = first;
+    if (!live) it.s = n_scen;
+    float us = it.s < n_scen ? u[v * ld_u + it.s] : 0.0f;
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
-    RowSums<double, NV> row;
-    row_sums<double, G, NV>(x, cut, g, row);
-    for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
-     for (int64_t s = beg; s < end; ++s) {
-      const float us = u[v * ld_u + s];
-      const double target = (double)fmaxf(us, 0.0f) * row.total;
-      int n = 0;
+    RowSums<float, NV> row;
+    row_sums<float, G, NV>(x, cut, g, row);
+    while (__any(it.s < n_scen)) {
+      const bool act = it.s < n_scen;
+      const int64_t s = it.s;
+      const float now = us;
+      it.next(a, n_scen);
+      us = it.s < n_scen ? u[v * ld_u + it.s] : 0.0f;
+      const float target = fmaxf(now, 0.0f) * row.total;
+      bool in[NV];
+      float near = kInf;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) n += row.c[j] <= target;
-      n = min(group_sum<G>(n), row.last);
-      if (g == 0) place[v * ld_place + s] = row.ok && us == us ? (uint16_t)n : kNoPlace;
-     }
-    });
+      for (int j = 0; j < NV; ++j) {
+        in[j] = row.c[j] <= target;
+        near = fminf(near, fabsf(row.c[j] - target));
+      }
+      const int n = min(group_count<G>(in), row.last);
+      const bool drawn = act && row.ok && now == now;
+      const bool unsure = drawn && (row.unsure || near <= kMargin * row.total);
+      const bool redo = group_umax<G>((uint32_t)unsure) != 0;
+      if (act && g == 0 && !redo) place[v * ld_place + s] = drawn ? (uint16_t)n : kNoPlace;
+      for (uint64_t left = __ballot(redo && g == 0); left; left &= left - 1) {
+        const int l = __builtin_ctzll(left);
+        const int64_t rv = from_lane(v, l);
+        const uint32_t at = draw_sure<kWide>(a, from_lane(pol, l), rv, from_lane(now, l));
+        if ((threadIdx.x & 63) == 0) place[rv * ld_place + from_lane(s, l)] = (uint16_t)at;
+      }
+    }
   }
 }
 
