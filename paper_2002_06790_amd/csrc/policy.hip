@@ -90,17 +90,57 @@ __device__ __forceinline__ int group_count(const bool (&f)[N]) {
   return G == 64 ? c : group_sum<G>(c);
 }
 
-// Sum over the lanes before this one, and over all of them.
+template <class T>
+__device__ __forceinline__ T from_lane(T v, int lane) {
+  uint32_t w[sizeof(T) / 4];
+  __builtin_memcpy(w, &v, sizeof(T));
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(T) / 4; ++i) w[i] = __builtin_amdgcn_readlane(w[i], lane);
+  __builtin_memcpy(&v, w, sizeof(T));
+  return v;
+}
+
+// v as the data-parallel move CTRL brings it to the lanes of ROWS and BANKS, 0 elsewhere.
+template <int CTRL, int ROWS, int BANKS, class F>
+__device__ __forceinline__ F moved(F v) {
+  uint32_t w[sizeof(F) / 4];
+  __builtin_memcpy(w, &v, sizeof(F));
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(F) / 4; ++i) w[i] = __builtin_amdgcn_update_dpp(0u, w[i], CTRL, ROWS, BANKS, false);
+  __builtin_memcpy(&v, w, sizeof(F));
+  return v;
+}
+
+// Sum over the lanes of a group before this one, and over all of them: shifts
+// within 16 lanes (0x110 + o), then the last lane of 16 (0x142) and of 32 (0x143)
+// passed on.  A shift brings other groups' values too; those are dropped.
 template <int G, class F>
 __device__ __forceinline__ F group_before(F v, int g, F &all) {
-  F in = v;
-#pragma unroll
-  for (int o = 1; o < G; o <<= 1) {
-    const F t = __shfl_up(in, o, G);
-    if (g >= o) in += t;
+  if constexpr (G == 1) {
+    all = v;
+    return F(0);
   }
-  all = __shfl(in, G - 1, G);
-  const F ex = __shfl_up(in, 1, G);
+  F in = v;
+  auto step = [&](F t, int o) { in += g % 16 >= o ? t : F(0); };
+  if constexpr (G > 1) step(moved<0x111, 0xF, 0xF>(in), 1);
+  if constexpr (G > 2) step(moved<0x112, 0xF, 0xF>(in), 2);
+  if constexpr (G > 4) step(moved<0x114, 0xF, 0xF>(in), 4);
+  if constexpr (G > 8) step(moved<0x118, 0xF, 0xF>(in), 8);
+  if constexpr (G > 16) in += moved<0x142, 0xA, 0xF>(in);
+  if constexpr (G > 32) in += moved<0x143, 0xC, 0xF>(in);
+  if constexpr (G == 2)
+    all = moved<0xF5, 0xF, 0xF>(in);  // quad 1 1 3 3
+  else if constexpr (G == 4)
+    all = moved<0xFF, 0xF, 0xF>(in);  // quad 3 3 3 3
+  else if constexpr (G == 64)
+    all = from_lane(in, 63);
+  else
+    all = __shfl(in, G - 1, G);
+  F ex;
+  if constexpr (G <= 16)
+    ex = moved<0x111, 0xF, 0xF>(in);
+  else
+    ex = __shfl_up(in, 1, G);
   return g ? ex : F(0);
 }
 
@@ -308,26 +348,17 @@ __device__ __forceinline__ void sort_row(float (&v)[NV], int g) {
   merge_up<1, G>(v, g);
 }
 
-// Partial sums of a row's kept weights w = exp((l - max) / T).  In 64 bits (F =
-// double) they are the definition; in 32 bits `unsure` says that a choice lies
-// within what the roundings can move: z carries five (its own, the reciprocal's, the
-// product with log2 e), so a weight is off by 2^-24 (5 |z| + 2) of itself and any
-// sum by the mean of that, where the mean |z| of a distribution over 1024 is at
-// most ln 1024; 22 additions and the product with u come on top: below 2^-17
-// of the whole sum, of which kMargin is twice.
-constexpr float kMargin = 0x1p-16f;
-
-template <class F, int NV>
+// Partial sums of a row's kept weights w = exp((l - max) / T), in 64 bits.
+template <int NV>
 struct RowSums {
-  F c[NV];  // up to and with this lane's resource j
-  F total;
-  int last;  // the last resource of positive weight
-  bool ok, unsure;
+  double c[NV];  // up to and with this lane's resource j
+  double total;
+  int last;      // the last resource of positive weight
+  bool ok;
 };
 
-template <class F, int G, int NV>
-__device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, int g, RowSums<F, NV> &out) {
-  constexpr bool kFast = sizeof(F) == 4;
+template <int G, int NV>
+__device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, int g, RowSums<NV> &out) {
   float m = x[0];
   int bad = 0;
 #pragma unroll
@@ -338,20 +369,11 @@ __device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, i
   m = group_max<G>(m);
   bad = group_sum<G>(bad);
   out.ok = !bad && cut.ok && m > -kInf && m < kInf;
-  const F inv = kFast ? F(1.44269504f * (1.0f / cut.T)) : F(1.0 / (double)cut.T);
-  int unsure = kFast && !(inv < F(1e30));
-  auto weight = [&](float l) -> F {
-    if constexpr (kFast)
-      return __builtin_amdgcn_exp2f((l - m) * inv);
-    else
-      return exp(((double)l - (double)m) * inv);
-  };
-  F w[NV];
+  const double inv = 1.0 / (double)cut.T;
+  auto weight = [&](float l) { return exp(((double)l - (double)m) * inv); };
+  double w[NV];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) w[j] = x[j] > -kInf ? weight(x[j]) : F(0);
-  uint32_t keep = 0;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) keep |= (x[j] > -kInf ? 1u : 0u) << j;
+  for (int j = 0; j < NV; ++j) w[j] = x[j] > -kInf ? weight(x[j]) : 0.0;
   if (cut.k < SIM_MAX_RES || cut.p < 1) {
     float s[NV];
 #pragma unroll
@@ -361,71 +383,158 @@ __device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, i
 #pragma unroll
     for (int j = 0; j < NV; ++j) in[j] = s[j] > -kInf && g * NV + j < cut.k;
     if (cut.p < 1) {
-      F ws[NV], mass = 0, all;
+      double ws[NV], mass = 0, all;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         ws[j] = mass;
-        mass += in[j] ? weight(s[j]) : F(0);
+        mass += in[j] ? weight(s[j]) : 0.0;
       }
-      const F before = group_before<G>(mass, g, all), target = (F)cut.p * all;
+      const double before = group_before<G>(mass, g, all), target = (double)cut.p * all;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const F b = ws[j] + before;
-        const bool first = g * NV + j == 0;
-        if constexpr (kFast) unsure |= in[j] && !first && fabsf(b - target) <= kMargin * all;
-        in[j] = in[j] && (b < target || first);
-      }
+      for (int j = 0; j < NV; ++j) in[j] = in[j] && (ws[j] + before < target || g * NV + j == 0);
     }
     // the last logit of the kept part, and how many of its equals belong to it
     float cutoff = kInf;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) cutoff = in[j] ? fminf(cutoff, s[j]) : cutoff;
+    for (int j = 0; j < NV; ++j) cutoff = in[j] ? s[j] : cutoff;
     cutoff = -group_max<G>(-cutoff);
-    bool eq[NV], eq_in[NV];
+    bool eq_in[NV];
+    int ties = 0, all;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      eq[j] = s[j] == cutoff;
-      eq_in[j] = eq[j] && in[j];
+      eq_in[j] = in[j] && s[j] == cutoff;
+      ties += x[j] == cutoff;
     }
     const int room = group_count<G>(eq_in);
-    keep = 0;
-    if (group_count<G>(eq) == room) {
+    int rank = group_before<G>(ties, g, all);
 #pragma unroll
-      for (int j = 0; j < NV; ++j) keep |= (x[j] >= cutoff ? 1u : 0u) << j;
+    for (int j = 0; j < NV; ++j) {
+      const bool tie = x[j] == cutoff;
+      if (!(x[j] > cutoff || (tie && rank < room))) w[j] = 0;
+      rank += tie;
+    }
+  }
+  double sum = 0;
+  int last = -1;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (w[j] < (double)cut.m) w[j] = 0;
+    sum += w[j];
+    out.c[j] = sum;
+    if (w[j] > 0) last = g * NV + j;
+  }
+  const double before = group_before<G>(sum, g, out.total);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) out.c[j] += before;
+  out.last = (int)group_umax<G>((uint32_t)(last + 1)) - 1;
+}
+
+// The same in 32 bits, where `unsure` says that a choice lies within what the
+// roundings can move: z = (l - max) / T carries five of them (its own, the reciprocal's,
+// the product with log2 e), so a weight is off by 2^-24 (5 |z| + 2) of itself
+// and a sum by the mean of that, where the mean |z| of a distribution over 1024 is at
+// most ln 1024; 22 additions and the product with u come on top: below 2^-17
+// of the whole sum, of which kMargin is twice.
+constexpr float kMargin = 0x1p-16f;
+
+template <int NV>
+struct RowNear {
+  float c[NV];
+  float total;  // NaN for a row without a distribution
+  bool unsure;  // of the group's lanes some may say so
+};
+
+template <int G, int NV>
+__device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, int g, RowNear<NV> &out) {
+  float m = x[0];
+#pragma unroll
+  for (int j = 1; j < NV; ++j) m = fmaxf(m, x[j]);
+  m = group_max<G>(m);
+  const float inv = 1.44269504f * (1.0f / cut.T);
+  bool unsure = !(inv < 1e30f);
+  auto weight = [&](float l) { return __builtin_amdgcn_exp2f((l - m) * inv); };
+  float w[NV], nan = cut.ok ? 0.0f : __builtin_nanf("");  // a row of -inf: the differences are NaN
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    w[j] = weight(x[j]);
+    nan += w[j];  // finite but for NaN
+  }
+  if (cut.k < SIM_MAX_RES || cut.p < 1) {
+    float s[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) s[j] = x[j];
+    sort_row<G, NV>(s, g);
+    const int k = cut.k - g * NV;  // so many of this lane's
+    float cutoff = s[0];
+    uint32_t kept = 0;
+    if (cut.p < 1) {
+      float ws[NV], mass = 0, all;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        ws[j] = mass;
+        mass += j < k ? weight(s[j]) : 0.0f;
+      }
+      const float before = group_before<G>(mass, g, all), target = cut.p * all;
+      float near = kInf;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const float off = ws[j] + before - target;
+        if (j > 0 || g > 0) near = fminf(near, j < k ? fabsf(off) : kInf);
+        const bool in = j < k && s[j] > -kInf && (off < 0 || (j == 0 && g == 0));
+        cutoff = in ? s[j] : cutoff;
+        kept += in;
+      }
+      unsure |= near <= kMargin * all;
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const bool in = j < k && s[j] > -kInf;
+        cutoff = in ? s[j] : cutoff;
+        kept += in;
+      }
+    }
+    cutoff = -group_max<G>(kept ? -cutoff : -kInf);
+    // as many at or above it as are kept, or some of its equals are not
+#pragma unroll
+    for (int j = 0; j < NV; ++j) kept += (x[j] >= cutoff ? 1u : 0u) << 16;
+    kept = group_sum<G>(kept);
+    if ((kept & 0xFFFFu) == kept >> 16) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) w[j] = x[j] >= cutoff ? w[j] : 0.0f;
     } else {
       int ties = 0, all;
 #pragma unroll
       for (int j = 0; j < NV; ++j) ties += x[j] == cutoff;
       int rank = group_before<G>(ties, g, all);
+      const int room = (int)(kept & 0xFFFFu) - ((int)(kept >> 16) - all);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const bool tie = x[j] == cutoff;
-        keep |= (x[j] > cutoff || (tie && rank < room) ? 1u : 0u) << j;
+        w[j] = x[j] > cutoff || (tie && rank < room) ? w[j] : 0.0f;
         rank += tie;
       }
     }
   }
   if (cut.m > 0) {
+    float near = kInf;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      if constexpr (kFast) unsure |= (keep >> j & 1) && fabsf(w[j] - cut.m) <= 0x1p-15f * cut.m;
-      if (w[j] < (F)cut.m) keep &= ~(1u << j);
+      near = fminf(near, fabsf(w[j] - cut.m));
+      w[j] = w[j] < cut.m ? 0.0f : w[j];
     }
+    unsure |= near <= 0x1p-15f * cut.m;
   }
-  F sum = 0;
-  int last = -1;
+  float sum = 0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const bool in = keep >> j & 1;
-    sum += in ? w[j] : F(0);
+    sum += w[j];
     out.c[j] = sum;
-    if (in && w[j] > 0) last = g * NV + j;
   }
-  const F before = group_before<G>(sum, g, out.total);
+  const float before = group_before<G>(sum, g, out.total);
 #pragma unroll
   for (int j = 0; j < NV; ++j) out.c[j] += before;
-  out.last = (int)group_umax<G>((uint32_t)(last + 1)) - 1;
-  if constexpr (kFast) out.unsure = group_umax<G>((uint32_t)unsure) != 0;
+  out.total += group_sum<G>(nan - nan);
+  out.unsure = unsure;
 }
 
 // A block's tile: 2^log_pol policies (or scenarios) by the groups left.
@@ -457,24 +566,14 @@ struct Scenarios {
   }
 };
 
-template <class T>
-__device__ __forceinline__ T from_lane(T v, int lane) {
-  uint32_t w[sizeof(T) / 4];
-  __builtin_memcpy(w, &v, sizeof(T));
-#pragma unroll
-  for (unsigned i = 0; i < sizeof(T) / 4; ++i) w[i] = __builtin_amdgcn_readlane(w[i], lane);
-  __builtin_memcpy(&v, w, sizeof(T));
-  return v;
-}
-
 // One draw in 64 bits by a whole wavefront.
 template <int NV>
 __device__ __forceinline__ uint32_t draw_sure(const PolicyArgs &a, int64_t pol, int64_t v, float u) {
   const int lane = threadIdx.x & 63;
   float x[NV];
   load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
-  RowSums<double, NV> row;
-  row_sums<double, 64, NV>(x, policy_cut(a, (int)pol), lane, row);
+  RowSums<NV> row;
+  row_sums<64, NV>(x, policy_cut(a, (int)pol), lane, row);
   const double target = (double)fmaxf(u, 0.0f) * row.total;
   bool in[NV];
 #pragma unroll
@@ -509,27 +608,23 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
     float us = it.s < n_scen ? u[v * ld_u + it.s] : 0.0f;
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
-    RowSums<float, NV> row;
-    row_sums<float, G, NV>(x, cut, g, row);
+    RowNear<NV> row;
+    row_near<G, NV>(x, cut, g, row);
     while (__any(it.s < n_scen)) {
       const bool act = it.s < n_scen;
       const int64_t s = it.s;
       const float now = us;
       it.next(a, n_scen);
       us = it.s < n_scen ? u[v * ld_u + it.s] : 0.0f;
-      const float target = fmaxf(now, 0.0f) * row.total;
-      bool in[NV];
-      float near = kInf;
+      // sure where as many sums lie below the target's margin as below its end, and not all
+      const float target = fmaxf(now, 0.0f) * row.total, margin = kMargin * row.total;
+      uint32_t n = row.unsure;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        in[j] = row.c[j] <= target;
-        near = fminf(near, fabsf(row.c[j] - target));
-      }
-      const int n = min(group_count<G>(in), row.last);
-      const bool drawn = act && row.ok && now == now;
-      const bool unsure = drawn && (row.unsure || near <= kMargin * row.total);
-      const bool redo = group_umax<G>((uint32_t)unsure) != 0;
-      if (act && g == 0 && !redo) place[v * ld_place + s] = drawn ? (uint16_t)n : kNoPlace;
+      for (int j = 0; j < NV; ++j) n += (row.c[j] <= target - margin ? 0x400u : 0u) + (row.c[j] <= target + margin ? 0x200000u : 0u);
+      n = group_sum<G>(n);
+      const bool drawn = act && row.total > 0 && now == now;
+      const bool redo = drawn && ((n & 0x3FFu) || (n >> 10 & 0x7FFu) != n >> 21 || n >> 21 == G * NV);
+      if (act && g == 0 && !redo) place[v * ld_place + s] = drawn ? (uint16_t)(n >> 21) : kNoPlace;
       for (uint64_t left = __ballot(redo && g == 0); left; left &= left - 1) {
         const int l = __builtin_ctzll(left);
         const int64_t rv = from_lane(v, l);
@@ -841,8 +936,8 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
   if (of_row == 0) {
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
-    RowSums<double, NV> row;
-    row_sums<double, 64, NV>(x, policy_cut(a, pc.pol), lane, row);
+    RowSums<NV> row;
+    row_sums<64, NV>(x, policy_cut(a, pc.pol), lane, row);
     const double inv = 1.0 / row.total;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
