@@ -20,11 +20,6 @@ int64_t extent(int64_t n_pol, int64_t n_ops, int64_t n, int64_t ld_pol, int64_t 
 
 bool aligned(const void *p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 
-bool rows_aligned(const void *p, int32_t dtype, int64_t ld_pol, int64_t ld_op) {
-  const int64_t per = 16 / elem_bytes(dtype);
-  return aligned(p, 16) && ld_pol % per == 0 && ld_op % per == 0;
-}
-
 // The checks every call makes, and the kernels' view of the policy.
 int make_policy(const sim_policy *p, int64_t n_scen, PolicyArgs &a) {
   if (!p || n_scen < 0) return SIM_E_INVAL;
@@ -59,7 +54,6 @@ int make_policy(const sim_policy *p, int64_t n_scen, PolicyArgs &a) {
   a.n_pol = p->n_pol;
   a.n_ops = p->n_ops;
   a.n_res = p->n_res;
-  a.vec = rows_aligned(p->logits, p->dtype, p->ld_pol, p->ld_op);
   return SIM_OK;
 }
 
@@ -72,7 +66,7 @@ int make_out(const PolicyArgs &a, void *grad, int64_t ld_pol, int64_t ld_op, Pol
   const bool by_pol = (one_op || ld_op >= a.n_res) && (one_pol || ld_pol >= ops);
   const bool by_op = (one_pol || ld_pol >= a.n_res) && (one_op || ld_op >= pols);
   if (!by_pol && !by_op) return SIM_E_INVAL;
-  out = PolicyOut{grad, ld_pol, ld_op, rows_aligned(grad, a.dtype, ld_pol, ld_op)};
+  out = PolicyOut{grad, ld_pol, ld_op};
   return SIM_OK;
 }
 

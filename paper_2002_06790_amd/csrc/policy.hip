@@ -100,13 +100,14 @@ __device__ __forceinline__ T from_lane(T v, int lane) {
   return v;
 }
 
-// v as the data-parallel move CTRL brings it to the lanes of ROWS and BANKS, 0 elsewhere.
-template <int CTRL, int ROWS, int BANKS, class F>
+// v as the data-parallel move CTRL brings it to the rows of 16 lanes in ROWS, 0 elsewhere.
+template <int CTRL, int ROWS, class F>
 __device__ __forceinline__ F moved(F v) {
   uint32_t w[sizeof(F) / 4];
   __builtin_memcpy(w, &v, sizeof(F));
 #pragma unroll
-  for (unsigned i = 0; i < sizeof(F) / 4; ++i) w[i] = __builtin_amdgcn_update_dpp(0u, w[i], CTRL, ROWS, BANKS, false);
+  for (unsigned i = 0; i < sizeof(F) / 4; ++i)
+    w[i] = ROWS == 0xF ? __builtin_amdgcn_mov_dpp(w[i], CTRL, 0xF, 0xF, true) : __builtin_amdgcn_update_dpp(0u, w[i], CTRL, ROWS, 0xF, false);
   __builtin_memcpy(&v, w, sizeof(F));
   return v;
 }
@@ -122,23 +123,23 @@ __device__ __forceinline__ F group_before(F v, int g, F &all) {
   }
   F in = v;
   auto step = [&](F t, int o) { in += g % 16 >= o ? t : F(0); };
-  if constexpr (G > 1) step(moved<0x111, 0xF, 0xF>(in), 1);
-  if constexpr (G > 2) step(moved<0x112, 0xF, 0xF>(in), 2);
-  if constexpr (G > 4) step(moved<0x114, 0xF, 0xF>(in), 4);
-  if constexpr (G > 8) step(moved<0x118, 0xF, 0xF>(in), 8);
-  if constexpr (G > 16) in += moved<0x142, 0xA, 0xF>(in);
-  if constexpr (G > 32) in += moved<0x143, 0xC, 0xF>(in);
+  if constexpr (G > 1) step(moved<0x111, 0xF>(in), 1);
+  if constexpr (G > 2) step(moved<0x112, 0xF>(in), 2);
+  if constexpr (G > 4) step(moved<0x114, 0xF>(in), 4);
+  if constexpr (G > 8) step(moved<0x118, 0xF>(in), 8);
+  if constexpr (G > 16) in += moved<0x142, 0xA>(in);
+  if constexpr (G > 32) in += moved<0x143, 0xC>(in);
   if constexpr (G == 2)
-    all = moved<0xF5, 0xF, 0xF>(in);  // quad 1 1 3 3
+    all = moved<0xF5, 0xF>(in);  // quad 1 1 3 3
   else if constexpr (G == 4)
-    all = moved<0xFF, 0xF, 0xF>(in);  // quad 3 3 3 3
+    all = moved<0xFF, 0xF>(in);  // quad 3 3 3 3
   else if constexpr (G == 64)
     all = from_lane(in, 63);
   else
     all = __shfl(in, G - 1, G);
   F ex;
   if constexpr (G <= 16)
-    ex = moved<0x111, 0xF, 0xF>(in);
+    ex = moved<0x111, 0xF>(in);
   else
     ex = __shfl_up(in, 1, G);
   return g ? ex : F(0);
@@ -177,68 +178,53 @@ __device__ __forceinline__ float load_elem(const void *base, int32_t dtype, int6
   return half_value(((const uint16_t *)base)[i], dtype == SIM_F16);
 }
 
-// x[j] = the row's element r0 + j, -inf behind its end.
+// x[j] = the row's element r0 + j, -inf behind its end.  Lanes with NV elements
+// take them in loads of 16 bytes, which need no alignment; only a row whose length NV
+// does not divide has a lane that takes fewer, one by one.
 template <int NV>
-__device__ __forceinline__ void load_row(const void *base, int32_t dtype, int64_t row, int r0, int n, bool vec,
-                                         float (&x)[NV]) {
-  if (dtype == SIM_F32) {
-    const float *p = (const float *)base + row + r0;
-    if (NV % 8 == 0 && vec && r0 + NV <= n) {
+__device__ __forceinline__ void load_row(const void *base, int32_t dtype, int64_t row, int r0, int n, float (&x)[NV]) {
 #pragma unroll
-      for (int j = 0; j + 3 < NV; j += 4) {
-        const float4 t = *(const float4 *)(p + j);
-        x[j] = t.x, x[j + 1] = t.y, x[j + 2] = t.z, x[j + 3] = t.w;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) x[j] = r0 + j < n ? p[j] : -kInf;
-    }
-    return;
-  }
-  const uint16_t *p = (const uint16_t *)base + row + r0;
+  for (int j = 0; j < NV; ++j) x[j] = -kInf;
   const bool f16 = dtype == SIM_F16;
-  if (NV % 8 == 0 && vec && r0 + NV <= n) {
+  if (r0 + NV <= n) {
+    if (dtype == SIM_F32) {
+      __builtin_memcpy(x, (const float *)base + row + r0, sizeof(x));
+    } else {
+      uint16_t h[NV];
+      __builtin_memcpy(h, (const uint16_t *)base + row + r0, sizeof(h));
 #pragma unroll
-    for (int j = 0; j + 7 < NV; j += 8) {
-      const uint4 t = *(const uint4 *)(p + j);
-      const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[j + i] = half_value((w[i / 2] >> (16 * (i & 1))) & 0xFFFFu, f16);
+      for (int j = 0; j < NV; ++j) x[j] = half_value(h[j], f16);
     }
-  } else {
+  }
+  if (NV > 1 && n % NV && r0 < n && r0 + NV > n) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) x[j] = r0 + j < n ? half_value(p[j], f16) : -kInf;
+    for (int j = 0; j < NV; ++j)
+      if (r0 + j < n) x[j] = load_elem(base, dtype, row + r0 + j);
   }
 }
 
 template <int NV>
-__device__ __forceinline__ void store_row(void *base, int32_t dtype, int64_t row, int r0, int n, bool vec,
-                                          const float (&x)[NV]) {
-  if (dtype == SIM_F32) {
-    float *p = (float *)base + row + r0;
-    if (NV % 8 == 0 && vec && r0 + NV <= n) {
+__device__ __forceinline__ void store_row(void *base, int32_t dtype, int64_t row, int r0, int n, const float (&x)[NV]) {
+  uint16_t h[NV];
+  if (dtype != SIM_F32) {
 #pragma unroll
-      for (int j = 0; j + 3 < NV; j += 4) *(float4 *)(p + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (r0 + j < n) p[j] = x[j];
-    }
-    return;
+    for (int j = 0; j < NV; ++j) h[j] = (uint16_t)(dtype == SIM_F16 ? f16_bits(x[j]) : bf16_bits(x[j]));
   }
-  uint16_t *p = (uint16_t *)base + row + r0;
-  uint32_t b[NV];
+  if (r0 + NV <= n) {
+    if (dtype == SIM_F32)
+      __builtin_memcpy((float *)base + row + r0, x, sizeof(x));
+    else
+      __builtin_memcpy((uint16_t *)base + row + r0, h, sizeof(h));
+  }
+  if (NV > 1 && n % NV && r0 < n && r0 + NV > n) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) b[j] = dtype == SIM_F16 ? f16_bits(x[j]) : bf16_bits(x[j]);
-  if (NV % 8 == 0 && vec && r0 + NV <= n) {
-#pragma unroll
-    for (int j = 0; j + 7 < NV; j += 8)
-      *(uint4 *)(p + j) = make_uint4(b[j] | b[j + 1] << 16, b[j + 2] | b[j + 3] << 16, b[j + 4] | b[j + 5] << 16,
-                                     b[j + 6] | b[j + 7] << 16);
-  } else {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (r0 + j < n) p[j] = (uint16_t)b[j];
+    for (int j = 0; j < NV; ++j) {
+      if (r0 + j >= n) continue;
+      if (dtype == SIM_F32)
+        ((float *)base)[row + r0 + j] = x[j];
+      else
+        ((uint16_t *)base)[row + r0 + j] = h[j];
+    }
   }
 }
 
@@ -311,28 +297,33 @@ __device__ __forceinline__ void merge_lanes(float (&v)[NV], int g) {
   if constexpr (S > 1) merge_lanes<S / 2>(v, g);
 }
 
+// A lane's bitonic values into falling order.
+template <int NV>
+__device__ __forceinline__ void merge_lane(float (&v)[NV]) {
+#pragma unroll
+  for (int s = NV / 2; s >= 1; s /= 2)
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (!(j & s)) {
+        const float hi = fmaxf(v[j], v[j + s]), lo = fminf(v[j], v[j + s]);
+        v[j] = hi, v[j + s] = lo;
+      }
+}
+
 // Merge the sorted halves of 2 L lanes: the bitonic order, all steps the same way.
 template <int L, int G, int NV>
 __device__ __forceinline__ void merge_up(float (&v)[NV], int g) {
   if constexpr (L < G) {
     exchange<2 * L - 1, true>(v, (g & L) ? -kInf : kInf);
     if constexpr (L > 1) merge_lanes<L / 2>(v, g);
-#pragma unroll
-    for (int s = NV / 2; s >= 1; s /= 2)
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (!(j & s)) {
-          const float hi = fmaxf(v[j], v[j + s]), lo = fminf(v[j], v[j + s]);
-          v[j] = hi, v[j + s] = lo;
-        }
+    merge_lane(v);
     merge_up<2 * L, G>(v, g);
   }
 }
 
-// Sort a group's G * NV values, the largest into element 0 of lane 0: the lanes'
-// own by the odd-even merge exchanges, then bitonic merges of lanes.
-template <int G, int NV>
-__device__ __forceinline__ void sort_row(float (&v)[NV], int g) {
+// A lane's values in falling order: the odd-even merge exchanges.
+template <int NV>
+__device__ __forceinline__ void sort_lane(float (&v)[NV]) {
 #pragma unroll
   for (int p = 1; p < NV; p *= 2)
 #pragma unroll
@@ -345,7 +336,27 @@ __device__ __forceinline__ void sort_row(float (&v)[NV], int g) {
             const float hi = fmaxf(v[i + j], v[i + j + k]), lo = fminf(v[i + j], v[i + j + k]);
             v[i + j] = hi, v[i + j + k] = lo;
           }
+}
+
+// Sort a group's G * NV values, the largest into element 0 of lane 0.
+template <int G, int NV>
+__device__ __forceinline__ void sort_row(float (&v)[NV], int g) {
+  sort_lane<NV>(v);
   merge_up<1, G>(v, g);
+}
+
+// The NV largest of a group in falling order, in every lane, from the lanes' own.
+template <int L, int G, int NV>
+__device__ __forceinline__ void merge_top(float (&v)[NV]) {
+  if constexpr (L < G) {
+    float q[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) q[j] = __uint_as_float(lane_xor<2 * L - 1>(__float_as_uint(v[NV - 1 - j])));
+#pragma unroll
+    for (int j = 0; j < NV; ++j) v[j] = fmaxf(v[j], q[j]);
+    merge_lane(v);
+    merge_top<2 * L, G>(v);
+  }
 }
 
 // Partial sums of a row's kept weights w = exp((l - max) / T), in 64 bits.
@@ -463,28 +474,35 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
     float s[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) s[j] = x[j];
-    sort_row<G, NV>(s, g);
-    const int k = cut.k - g * NV;  // so many of this lane's
+    // up to NV resources kept: every lane gets them all, from a shorter merge
+    const bool top = G > 1 && cut.k <= NV;
+    sort_lane<NV>(s);
+    if (top)
+      merge_top<1, G>(s);
+    else
+      merge_up<1, G>(s, g);
+    const int k = top ? cut.k : cut.k - g * NV;  // so many of this lane's
+    const bool head = top || g == 0;             // element 0 is the first of the order
     float cutoff = s[0];
     uint32_t kept = 0;
     if (cut.p < 1) {
-      float ws[NV], mass = 0, all;
+      float ws[NV], mass = 0, before = 0, near = kInf;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         ws[j] = mass;
         mass += j < k ? weight(s[j]) : 0.0f;
       }
-      const float before = group_before<G>(mass, g, all), target = cut.p * all;
-      float near = kInf;
+      if (!top) before = group_before<G>(mass, g, mass);
+      const float target = cut.p * mass;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const float off = ws[j] + before - target;
-        if (j > 0 || g > 0) near = fminf(near, j < k ? fabsf(off) : kInf);
-        const bool in = j < k && s[j] > -kInf && (off < 0 || (j == 0 && g == 0));
+        if (j > 0 || !head) near = fminf(near, j < k ? fabsf(off) : kInf);
+        const bool in = j < k && s[j] > -kInf && (off < 0 || (j == 0 && head));
         cutoff = in ? s[j] : cutoff;
         kept += in;
       }
-      unsure |= near <= kMargin * all;
+      unsure |= near <= kMargin * mass;
     } else {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -494,6 +512,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
       }
     }
     cutoff = -group_max<G>(kept ? -cutoff : -kInf);
+    if (top && g) kept = 0;  // counted in lane 0
     // as many at or above it as are kept, or some of its equals are not
 #pragma unroll
     for (int j = 0; j < NV; ++j) kept += (x[j] >= cutoff ? 1u : 0u) << 16;
@@ -568,12 +587,12 @@ struct Scenarios {
 
 // One draw in 64 bits by a whole wavefront.
 template <int NV>
-__device__ __forceinline__ uint32_t draw_sure(const PolicyArgs &a, int64_t pol, int64_t v, float u) {
+__device__ __noinline__ uint32_t draw_sure(const PolicyArgs &a, int pol, int64_t at_row, float u) {
   const int lane = threadIdx.x & 63;
   float x[NV];
-  load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
+  load_row<NV>(a.logits, a.dtype, at_row, lane * NV, a.n_res, x);
   RowSums<NV> row;
-  row_sums<64, NV>(x, policy_cut(a, (int)pol), lane, row);
+  row_sums<64, NV>(x, policy_cut(a, pol), lane, row);
   const double target = (double)fmaxf(u, 0.0f) * row.total;
   bool in[NV];
 #pragma unroll
@@ -599,15 +618,19 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
   const Cut cut = policy_cut(a, (int)pol);
   Scenarios first;
   first.begin(a, pol, n_scen);
-  for (int i = 0; i < t.per; ++i) {
-    const bool live = live_pol && v0 + (int64_t)i * nv < a.n_ops;
+  if (!live_pol) first.s = n_scen;
+  int64_t v = live_pol ? v0 : a.n_ops;
+  // unsigned: what is past the last op may wrap, and is not used
+  uint64_t at_row = (uint64_t)pol * a.ld_pol + (uint64_t)v0 * a.ld_op, at_u = (uint64_t)v0 * ld_u, at_place = (uint64_t)v0 * ld_place;
+  for (int i = 0; i < t.per; ++i, v += nv, at_row += nv * a.ld_op, at_u += nv * ld_u, at_place += nv * ld_place) {
+    const bool live = v < a.n_ops;
     if (!__any(live)) return;
-    const int64_t v = live ? v0 + (int64_t)i * nv : 0;
     Scenarios it = first;
     if (!live) it.s = n_scen;
-    float us = it.s < n_scen ? u[v * ld_u + it.s] : 0.0f;
+    const float *pu = u + at_u;
+    float us = it.s < n_scen ? pu[it.s] : 0.0f;
     float x[NV];
-    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
+    load_row<NV>(a.logits, a.dtype, live ? (int64_t)at_row : 0, g * NV, a.n_res, x);
     RowNear<NV> row;
     row_near<G, NV>(x, cut, g, row);
     while (__any(it.s < n_scen)) {
@@ -615,7 +638,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
       const int64_t s = it.s;
       const float now = us;
       it.next(a, n_scen);
-      us = it.s < n_scen ? u[v * ld_u + it.s] : 0.0f;
+      us = it.s < n_scen ? pu[it.s] : 0.0f;
       // sure where as many sums lie below the target's margin as below its end, and not all
       const float target = fmaxf(now, 0.0f) * row.total, margin = kMargin * row.total;
       uint32_t n = row.unsure;
@@ -624,12 +647,11 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
       n = group_sum<G>(n);
       const bool drawn = act && row.total > 0 && now == now;
       const bool redo = drawn && ((n & 0x3FFu) || (n >> 10 & 0x7FFu) != n >> 21 || n >> 21 == G * NV);
-      if (act && g == 0 && !redo) place[v * ld_place + s] = drawn ? (uint16_t)(n >> 21) : kNoPlace;
+      if (act && g == 0 && !redo) place[at_place + s] = drawn ? (uint16_t)(n >> 21) : kNoPlace;
       for (uint64_t left = __ballot(redo && g == 0); left; left &= left - 1) {
         const int l = __builtin_ctzll(left);
-        const int64_t rv = from_lane(v, l);
-        const uint32_t at = draw_sure<kWide>(a, from_lane(pol, l), rv, from_lane(now, l));
-        if ((threadIdx.x & 63) == 0) place[rv * ld_place + from_lane(s, l)] = (uint16_t)at;
+        const uint32_t at = draw_sure<kWide>(a, from_lane((int32_t)pol, l), (int64_t)from_lane(at_row, l), from_lane(now, l));
+        if ((threadIdx.x & 63) == 0) place[from_lane(at_place + s, l)] = (uint16_t)at;
       }
     }
   }
@@ -684,7 +706,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t 
       const int64_t v = chunk * nv * t.per + (int64_t)i * nv + (grp >> t.log_pol);
       if (v >= a.n_ops) break;
       float x[NV];
-      load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
+      load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, x);
       RowExp<NV> row;
       row_exp<G, NV>(x, T, row);
       const int at = place[v * ld_place + s];
@@ -803,7 +825,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp_runs(PolicyArgs a, int
     load(0);
     if (grp < rows) {
       float x[NV];
-      load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + (v0 + grp) * a.ld_op, g * NV, R, a.vec, x);
+      load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + (v0 + grp) * a.ld_op, g * NV, R, x);
       RowExp<NV> row;
       row_exp<G, NV>(x, T, row);
       const float ls = logf(row.sum);
@@ -935,7 +957,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
   load();
   if (of_row == 0) {
     float x[NV];
-    load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, a.vec, x);
+    load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, x);
     RowSums<NV> row;
     row_sums<64, NV>(x, policy_cut(a, pc.pol), lane, row);
     const double inv = 1.0 / row.total;
@@ -1014,7 +1036,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
     const int64_t v = v0 + (int64_t)i * nv;
     if (v >= a.n_ops) return;
     float x[NV], h[NV], out[NV];
-    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, a.vec, x);
+    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, x);
     RowExp<NV> row;
     row_exp<G, NV>(x, T, row);
 #pragma unroll
@@ -1028,7 +1050,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
      }
     });
     row_grad<G, NV>(row, T, h, out);
-    store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g * NV, a.n_res, grad.vec, out);
+    store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g * NV, a.n_res, out);
   }
 }
 
@@ -1092,7 +1114,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
   const bool finish = own < rows;
   float x[NV];
   if (finish && splits == 1)
-    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, lane * NV, R, a.vec, x);
+    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, lane * NV, R, x);
   for (int i = t; i < RB * R * C; i += 64 * WR) table[i] = 0;
   const float top = group_max<64>(peak[lane]);
   // adding and taking away 1.5 2^52 grid steps rounds to the grid
@@ -1199,7 +1221,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
   RowExp<NV> row;
   row_exp<64, NV>(x, T, row);
   row_grad<64, NV>(row, T, h, out);
-  store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, R, grad.vec, out);
+  store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, R, out);
 }
 
 // The splits' sums of every row joined in order, and its gradient.
@@ -1212,7 +1234,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, con
   const uint32_t pol = row_id / (uint32_t)a.n_ops, v = row_id - pol * (uint32_t)a.n_ops;
   const float T = policy_temperature(a, (int)pol);
   float x[NV], h[NV], out[NV];
-  load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, a.n_res, a.vec, x);
+  load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, a.n_res, x);
   double sum[NV] = {};
   for (uint32_t k = 0; k < splits; ++k) {
     const double *p = part + ((int64_t)k * rows + row_id) * a.n_res + r0;
@@ -1224,7 +1246,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, con
   RowExp<NV> row;
   row_exp<G, NV>(x, T, row);
   row_grad<G, NV>(row, T, h, out);
-  store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, grad.vec, out);
+  store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, out);
 }
 
 template <int G, int NV>
@@ -1240,7 +1262,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
     const int64_t pol = row_id / a.n_ops, v = row_id - pol * a.n_ops;
     const float T = policy_temperature(a, (int)pol);
     float x[NV];
-    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, a.n_res, a.vec, x);
+    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, a.n_res, x);
     RowExp<NV> row;
     row_exp<G, NV>(x, T, row);
     const uint16_t *ids = top.res + pol * top.ld_res_pol + v * top.ld_res_op;
@@ -1306,7 +1328,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
 #pragma unroll
         for (int j = 0; j < NV; ++j) out[j] = nan;
       }
-      store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, grad.vec, out);
+      store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, out);
     }
     wave_order();
   }

@@ -20,14 +20,12 @@ struct PolicyArgs {
   float temperature, top_k, top_p, min_p;
   int32_t dtype;
   int32_t n_pol, n_ops, n_res;
-  int32_t vec;              // 1: every row begins at a multiple of 16 bytes
 };
 
 // Gradient rows: same shape and type as the logits, strides of their own.
 struct PolicyOut {
   void *p;
   int64_t ld_pol, ld_op;
-  int32_t vec;
 };
 
 // A teacher's table: K resources and logits per op and policy.
