@@ -455,7 +455,7 @@ struct RowNear {
   bool unsure;  // of the group's lanes some may say so
 };
 
-template <int G, int NV>
+template <int G, int NV, bool CUT>
 __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, int g, RowNear<NV> &out) {
   float m = x[0];
 #pragma unroll
@@ -468,9 +468,9 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     w[j] = weight(x[j]);
-    nan += w[j];  // finite but for NaN
+    if (CUT) nan += w[j];  // finite but for NaN; without a cut the sums show it
   }
-  if (cut.k < SIM_MAX_RES || cut.p < 1) {
+  if (CUT && (cut.k < SIM_MAX_RES || cut.p < 1)) {
     float s[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) s[j] = x[j];
@@ -534,7 +534,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
       }
     }
   }
-  if (cut.m > 0) {
+  if (CUT && cut.m > 0) {
     float near = kInf;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -552,7 +552,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
   const float before = group_before<G>(sum, g, out.total);
 #pragma unroll
   for (int j = 0; j < NV; ++j) out.c[j] += before;
-  out.total += group_sum<G>(nan - nan);
+  out.total += CUT ? group_sum<G>(nan - nan) : nan;
   out.unsure = unsure;
 }
 
@@ -600,59 +600,75 @@ __device__ __noinline__ uint32_t draw_sure(const PolicyArgs &a, int pol, int64_t
   return min(group_count<64>(in), row.last);
 }
 
-// Few scenarios a row: a group of lanes works a row out in 32 bits and draws
-// its scenarios one after another.  A draw that lies within the roundings of a border
-// (about one in a thousand at 64 resources) is done again in 64 bits by the
-// whole wavefront, so that every answer is the 64-bit one.
-template <int G, int NV>
+// The scenario of a policy that has at most one; n_scen when it has none.
+__device__ __forceinline__ int64_t only_scenario(const PolicyArgs &a, int64_t pol, int64_t n_scen) {
+  const int64_t s = pol >= a.phase ? pol - a.phase : pol - a.phase + a.period;
+  return s < n_scen ? s : n_scen;
+}
+
+// Few scenarios a row (ONE: at most one): a group of lanes works a row out in
+// 32 bits and draws its scenarios one after another.  A draw that lies within
+// the roundings of a border (about one in a thousand at 64 resources) is done
+// again in 64 bits by the whole wavefront, so that every answer is the 64-bit one.
+template <int G, int NV, bool CUT, bool ONE>
 __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
                                                             uint16_t *place, int64_t ld_place, Tile t) {
   constexpr int kWide = G * NV > 64 ? G * NV / 64 : 1;
   const int g = threadIdx.x % G, grp = threadIdx.x / G;
   const int np = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
-  const int64_t pol_tiles = (a.n_pol + np - 1) / np;
-  const int64_t pol_at = blockIdx.x % pol_tiles * np + (grp & (np - 1));
-  const int64_t v0 = blockIdx.x / pol_tiles * (int64_t)nv * t.per + (grp >> t.log_pol);
-  const bool live_pol = pol_at < a.n_pol;
-  const int64_t pol = live_pol ? pol_at : 0;
-  const Cut cut = policy_cut(a, (int)pol);
+  const uint32_t pol_tiles = ((uint32_t)a.n_pol + np - 1) >> t.log_pol, v_tile = blockIdx.x / pol_tiles;
+  const uint32_t pol_at = ((blockIdx.x - v_tile * pol_tiles) << t.log_pol) + (grp & (np - 1));
+  const int64_t v0 = (int64_t)v_tile * nv * t.per + (grp >> t.log_pol);
+  const bool live_pol = pol_at < (uint32_t)a.n_pol;
+  const int pol = live_pol ? (int)pol_at : 0;
+  const Cut cut = policy_cut(a, pol);
   Scenarios first;
-  first.begin(a, pol, n_scen);
+  if (ONE)
+    first.s = only_scenario(a, pol, n_scen);
+  else
+    first.begin(a, pol, n_scen);
   if (!live_pol) first.s = n_scen;
-  int64_t v = live_pol ? v0 : a.n_ops;
   // unsigned: what is past the last op may wrap, and is not used
   uint64_t at_row = (uint64_t)pol * a.ld_pol + (uint64_t)v0 * a.ld_op, at_u = (uint64_t)v0 * ld_u, at_place = (uint64_t)v0 * ld_place;
-  for (int i = 0; i < t.per; ++i, v += nv, at_row += nv * a.ld_op, at_u += nv * ld_u, at_place += nv * ld_place) {
-    const bool live = v < a.n_ops;
-    if (!__any(live)) return;
+  const int steps = (int)min((int64_t)t.per, (a.n_ops - v0 + nv - 1) / nv);  // of this group
+  for (int i = 0; __any(i < steps); ++i, at_row += nv * a.ld_op, at_u += nv * ld_u, at_place += nv * ld_place) {
     Scenarios it = first;
-    if (!live) it.s = n_scen;
+    if (i >= steps) it.s = n_scen;
     const float *pu = u + at_u;
     float us = it.s < n_scen ? pu[it.s] : 0.0f;
     float x[NV];
-    load_row<NV>(a.logits, a.dtype, live ? (int64_t)at_row : 0, g * NV, a.n_res, x);
+    load_row<NV>(a.logits, a.dtype, i < steps ? (int64_t)at_row : 0, g * NV, a.n_res, x);
     RowNear<NV> row;
-    row_near<G, NV>(x, cut, g, row);
+    row_near<G, NV, CUT>(x, cut, g, row);
+    const float margin = kMargin * row.total;
     while (__any(it.s < n_scen)) {
       const bool act = it.s < n_scen;
       const int64_t s = it.s;
       const float now = us;
-      it.next(a, n_scen);
-      us = it.s < n_scen ? pu[it.s] : 0.0f;
+      if (ONE) {
+        it.s = n_scen;
+      } else {
+        it.next(a, n_scen);
+        us = it.s < n_scen ? pu[it.s] : 0.0f;
+      }
       // sure where as many sums lie below the target's margin as below its end, and not all
-      const float target = fmaxf(now, 0.0f) * row.total, margin = kMargin * row.total;
-      uint32_t n = row.unsure;
+      const float target = fmaxf(now, 0.0f) * row.total, from = target - margin, to = target + margin;
+      uint32_t below = 0, upto = 0;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) n += (row.c[j] <= target - margin ? 0x400u : 0u) + (row.c[j] <= target + margin ? 0x200000u : 0u);
-      n = group_sum<G>(n);
+      for (int j = 0; j < NV; ++j) {
+        below += row.c[j] <= from;
+        upto += row.c[j] <= to;
+      }
+      const uint32_t n = group_sum<G>(row.unsure + (below << 10) + (upto << 21));
       const bool drawn = act && row.total > 0 && now == now;
       const bool redo = drawn && ((n & 0x3FFu) || (n >> 10 & 0x7FFu) != n >> 21 || n >> 21 == G * NV);
       if (act && g == 0 && !redo) place[at_place + s] = drawn ? (uint16_t)(n >> 21) : kNoPlace;
       for (uint64_t left = __ballot(redo && g == 0); left; left &= left - 1) {
         const int l = __builtin_ctzll(left);
-        const uint32_t at = draw_sure<kWide>(a, from_lane((int32_t)pol, l), (int64_t)from_lane(at_row, l), from_lane(now, l));
+        const uint32_t at = draw_sure<kWide>(a, from_lane(pol, l), (int64_t)from_lane(at_row, l), from_lane(now, l));
         if ((threadIdx.x & 63) == 0) place[from_lane(at_place + s, l)] = (uint16_t)at;
       }
+      if (ONE) break;
     }
   }
 }
@@ -1467,9 +1483,9 @@ GradRuns grad_runs(const PolicyArgs &a, int64_t n_scen) {
 
 int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, int64_t ld_u, uint16_t *place,
                          int64_t ld_place, hipStream_t st) {
+  const bool cut = a.settings || a.temperature == 0 || a.top_k >= 1 || a.top_p < 1 || a.min_p > 0;
   if (std::min(a.block, n_scen) >= kLongRun) {
     Pieces ps;
-    const bool cut = a.settings || a.top_k >= 1 || a.top_p < 1 || a.min_p > 0;
     const int wr = !cut && std::min(a.block, n_scen) >= 2048 ? 4 : 1;
     const int64_t pieces = make_pieces(a, n_scen, wr > 1 ? 8192 : 4096, ps), blocks = pieces * ((a.n_ops * (int64_t)wr + 3) / 4);
     if (blocks > kMaxBlocks) return SIM_E_LIMIT;
@@ -1486,8 +1502,14 @@ int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, in
   int64_t blocks;
   if (int rc = row_tile(a, t, blocks)) return rc;
   return by_row(a.n_res, [&](auto G, auto NV) {
-    k_policy_sample<G(), NV()><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, t);
-    return launched();
+    auto go = [&](auto cuts, auto one) {
+      k_policy_sample<G(), NV(), cuts(), one()><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, t);
+      return launched();
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    const bool one = a.block == 1 && n_scen <= a.period;
+    return cut ? one ? go(yes, yes) : go(yes, no) : one ? go(no, yes) : go(no, no);
   });
 }
 
