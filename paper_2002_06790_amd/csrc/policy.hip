@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr float kInf = __builtin_inff();
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr uint16_t kNoPlace = 65535;
 
 // ---- values across the lanes of a group ----
@@ -160,16 +161,21 @@ __device__ __forceinline__ float f16_value(uint32_t bits) {
   __builtin_memcpy(&h, &b, 2);
   return (float)h;
 }
-// Round to nearest, ties to even; NaN stays NaN.
-__device__ __forceinline__ uint32_t bf16_bits(float x) {
-  const uint32_t b = __float_as_uint(x);
-  return x != x ? 0x7FC0u : (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
-}
-__device__ __forceinline__ uint32_t f16_bits(float x) {
-  const _Float16 h = (_Float16)x;
-  uint16_t b;
-  __builtin_memcpy(&b, &h, 2);
-  return b;
+// Both round to nearest, ties to even; NaN stays NaN.
+typedef __bf16 bf16_pair __attribute__((ext_vector_type(2)));
+typedef _Float16 f16_pair __attribute__((ext_vector_type(2)));
+typedef float f32_pair __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi, bool f16) {
+  const f32_pair v = {lo, hi};
+  uint32_t bits;
+  if (f16) {
+    const f16_pair h = __builtin_convertvector(v, f16_pair);
+    __builtin_memcpy(&bits, &h, 4);
+  } else {
+    const bf16_pair h = __builtin_convertvector(v, bf16_pair);
+    __builtin_memcpy(&bits, &h, 4);
+  }
+  return bits;
 }
 __device__ __forceinline__ float half_value(uint32_t bits, bool f16) { return f16 ? f16_value(bits) : bf16_value(bits); }
 
@@ -205,26 +211,28 @@ __device__ __forceinline__ void load_row(const void *base, int32_t dtype, int64_
 
 template <int NV>
 __device__ __forceinline__ void store_row(void *base, int32_t dtype, int64_t row, int r0, int n, const float (&x)[NV]) {
-  uint16_t h[NV];
-  if (dtype != SIM_F32) {
+  if (r0 >= n) return;
+  if (dtype == SIM_F32) {
+    float *p = (float *)base + row + r0;
+    if (r0 + NV <= n) {
+      __builtin_memcpy(p, x, sizeof(x));
+    } else {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) h[j] = (uint16_t)(dtype == SIM_F16 ? f16_bits(x[j]) : bf16_bits(x[j]));
-  }
-  if (r0 + NV <= n) {
-    if (dtype == SIM_F32)
-      __builtin_memcpy((float *)base + row + r0, x, sizeof(x));
-    else
-      __builtin_memcpy((uint16_t *)base + row + r0, h, sizeof(h));
-  }
-  if (NV > 1 && n % NV && r0 < n && r0 + NV > n) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      if (r0 + j >= n) continue;
-      if (dtype == SIM_F32)
-        ((float *)base)[row + r0 + j] = x[j];
-      else
-        ((uint16_t *)base)[row + r0 + j] = h[j];
+      for (int j = 0; j < NV; ++j)
+        if (r0 + j < n) p[j] = x[j];
     }
+    return;
+  }
+  uint16_t *p = (uint16_t *)base + row + r0;
+  uint32_t w[(NV + 1) / 2];
+#pragma unroll
+  for (int j = 0; j < NV; j += 2) w[j / 2] = half_pair(x[j], j + 1 < NV ? x[j + 1] : 0.0f, dtype == SIM_F16);
+  if (r0 + NV <= n) {
+    __builtin_memcpy(p, w, NV * 2);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (r0 + j < n) p[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
   }
 }
 
@@ -441,18 +449,19 @@ __device__ __forceinline__ void row_sums(const float (&x)[NV], const Cut &cut, i
 }
 
 // The same in 32 bits, where `unsure` says that a choice lies within what the
-// roundings can move: z = (l - max) / T carries five of them (its own, the reciprocal's,
-// the product with log2 e), so a weight is off by 2^-24 (5 |z| + 2) of itself
-// and a sum by the mean of that, where the mean |z| of a distribution over 1024 is at
-// most ln 1024; 22 additions and the product with u come on top: below 2^-17
+// roundings can move.  An exponent (l c - mc, below) carries four of them, so a
+// weight is off by 2^-24 (4 |z| + 2) of itself and a sum by the mean of that,
+// where the mean |z| of a distribution over 1024 is at most ln 1024; 22
+// additions, two differences and the product with u come on top: below 2^-17
 // of the whole sum, of which kMargin is twice.
 constexpr float kMargin = 0x1p-16f;
 
 template <int NV>
 struct RowNear {
-  float c[NV];
-  float total;  // NaN for a row without a distribution
-  bool unsure;  // of the group's lanes some may say so
+  float c[NV];   // within the lane
+  float before;  // of the lanes before
+  float total;   // NaN for a row without a distribution, or one that 32 bits cannot weigh
+  bool unsure;   // of the group's lanes some may say so
 };
 
 template <int G, int NV, bool CUT>
@@ -461,10 +470,11 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
 #pragma unroll
   for (int j = 1; j < NV; ++j) m = fmaxf(m, x[j]);
   m = group_max<G>(m);
-  const float inv = 1.44269504f * (1.0f / cut.T);
-  bool unsure = !(inv < 1e30f);
-  auto weight = [&](float l) { return __builtin_amdgcn_exp2f((l - m) * inv); };
-  float w[NV], nan = cut.ok ? 0.0f : __builtin_nanf("");  // a row of -inf: the differences are NaN
+  const float c = kLog2e * (1.0f / cut.T), mc = m * c;
+  bool unsure = !(fabsf(mc) < 65536.0f) && m > -kInf;
+  auto weight = [&](float l) { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, c, -mc)); };
+  const float most = weight(m);  // 1 but for the rounding of mc, in every weight alike
+  float w[NV], nan = cut.ok ? 0.0f : __builtin_nanf("");  // a row of -inf: the weights are NaN
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     w[j] = weight(x[j]);
@@ -535,13 +545,14 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
     }
   }
   if (CUT && cut.m > 0) {
+    const float least = cut.m * most;
     float near = kInf;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      near = fminf(near, fabsf(w[j] - cut.m));
-      w[j] = w[j] < cut.m ? 0.0f : w[j];
+      near = fminf(near, fabsf(w[j] - least));
+      w[j] = w[j] < least ? 0.0f : w[j];
     }
-    unsure |= near <= 0x1p-15f * cut.m;
+    unsure |= near <= 0x1p-15f * least;
   }
   float sum = 0;
 #pragma unroll
@@ -549,9 +560,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
     sum += w[j];
     out.c[j] = sum;
   }
-  const float before = group_before<G>(sum, g, out.total);
-#pragma unroll
-  for (int j = 0; j < NV; ++j) out.c[j] += before;
+  out.before = group_before<G>(sum, g, out.total);
   out.total += CUT ? group_sum<G>(nan - nan) : nan;
   out.unsure = unsure;
 }
@@ -597,7 +606,7 @@ __device__ __noinline__ uint32_t draw_sure(const PolicyArgs &a, int pol, int64_t
   bool in[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) in[j] = row.c[j] <= target;
-  return min(group_count<64>(in), row.last);
+  return row.ok ? min(group_count<64>(in), row.last) : kNoPlace;
 }
 
 // The scenario of a policy that has at most one; n_scen when it has none.
@@ -652,7 +661,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
         us = it.s < n_scen ? pu[it.s] : 0.0f;
       }
       // sure where as many sums lie below the target's margin as below its end, and not all
-      const float target = fmaxf(now, 0.0f) * row.total, from = target - margin, to = target + margin;
+      const float target = fmaxf(now, 0.0f) * row.total, mid = target - row.before, from = mid - margin, to = mid + margin;
       uint32_t below = 0, upto = 0;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -660,7 +669,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
         upto += row.c[j] <= to;
       }
       const uint32_t n = group_sum<G>(row.unsure + (below << 10) + (upto << 21));
-      const bool drawn = act && row.total > 0 && now == now;
+      const bool drawn = act && (row.total > 0 || (n & 0x3FFu)) && now == now;
       const bool redo = drawn && ((n & 0x3FFu) || (n >> 10 & 0x7FFu) != n >> 21 || n >> 21 == G * NV);
       if (act && g == 0 && !redo) place[at_place + s] = drawn ? (uint16_t)(n >> 21) : kNoPlace;
       for (uint64_t left = __ballot(redo && g == 0); left; left &= left - 1) {
@@ -673,36 +682,53 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample(PolicyArgs a, int64_
   }
 }
 
-// A row's softmax in 32 bits: z = (l - max) / T, e = exp z, their sum.  exp z
-// is the machine's 2^(z log2 e), off by 2^-24 (2 |z| + 2) of itself beside z's
-// own roundings: below what the sum's logarithm and its ratios carry anyway.
+// A row's weights in 32 bits, e = 2^(x c - mc) with c = log2 e / T and mc the
+// rounded product of c and the maximum m: one multiply-add and the machine's
+// 2^x.  What mc's rounding leaves in the exponent is the same for the whole row
+// (`shift`), so that ratios do not have it.  Where mc is so large that `shift`
+// might not be small, the difference is taken first.
+
+template <int NV>
+__device__ __forceinline__ void row_weights(const float (&x)[NV], float m, float c, float (&e)[NV], float &shift) {
+  const float mc = m * c;
+  const bool far = !(fabsf(mc) < 65536.0f);
+  shift = 0;
+  if (__any(far)) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) e[j] = x[j] == -kInf ? 0.0f : __builtin_amdgcn_exp2f((x[j] - m) * c);  // inf - inf: NaN
+  } else {
+    shift = __builtin_fmaf(m, c, -mc);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], c, -mc));
+  }
+}
+
+// A row's softmax in 32 bits.
 template <int NV>
 struct RowExp {
-  float z[NV], e[NV];
-  float sum;   // NaN for an invalid row
-  bool empty;
+  float e[NV];
+  float sum;     // of e; NaN for an invalid row, 0 for an empty one
+  float m, inv;  // the maximum, 1 / T
+  float shift;
+
+  // log pi of a resource with logit l: (l - m) / T is off by 2^-24 of 3 |z|.
+  __device__ __forceinline__ float log_sum() const { return kLn2 * (__builtin_amdgcn_logf(sum) - shift); }
+  __device__ __forceinline__ float z(float l) const { return (l - m) * inv; }
 };
 
 template <int G, int NV>
 __device__ __forceinline__ void row_exp(const float (&x)[NV], float T, RowExp<NV> &o) {
-  float m = x[0];
+  o.m = x[0];
 #pragma unroll
-  for (int j = 1; j < NV; ++j) m = fmaxf(m, x[j]);
-  m = group_max<G>(m);
-  float nan = 0;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) nan = x[j] != x[j] ? x[j] : nan;  // the maximum passes over NaN
+  for (int j = 1; j < NV; ++j) o.m = fmaxf(o.m, x[j]);
+  o.m = group_max<G>(o.m);
+  o.inv = 1.0f / T;
+  row_weights<NV>(x, o.m, o.inv * kLog2e, o.e, o.shift);
   float s = 0;
-  const float inv = 1.0f / T;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    o.z[j] = x[j] == -kInf ? -kInf : (x[j] - m) * inv;  // inf - inf: NaN
-    o.e[j] = __builtin_amdgcn_exp2f(o.z[j] * 1.44269504f);
-    s += o.e[j];
-  }
-  o.sum = group_sum<G>(s + nan);
+  for (int j = 0; j < NV; ++j) s += o.e[j];
+  o.sum = group_sum<G>(s);
   if (!(T > 0 && T < kInf)) o.sum = __builtin_nanf("");
-  o.empty = m == -kInf && o.sum == o.sum;
 }
 
 template <int G, int NV>
@@ -718,20 +744,20 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t 
   if (s < n_scen) {
     const int pol = policy_of(a, s);
     const float T = policy_temperature(a, pol);
-    for (int i = 0; i < t.per; ++i) {
-      const int64_t v = chunk * nv * t.per + (int64_t)i * nv + (grp >> t.log_pol);
-      if (v >= a.n_ops) break;
+    const int64_t v0 = chunk * nv * t.per + (grp >> t.log_pol);
+    uint64_t at_row = (uint64_t)pol * a.ld_pol + (uint64_t)v0 * a.ld_op, at_place = (uint64_t)v0 * ld_place + s;
+    const int steps = (int)min((int64_t)t.per, (a.n_ops - v0 + nv - 1) / nv);
+    for (int i = 0; i < steps; ++i, at_row += nv * a.ld_op, at_place += nv * ld_place) {
       float x[NV];
-      load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, x);
+      const int at = place[at_place];
+      load_row<NV>(a.logits, a.dtype, at_row, g * NV, a.n_res, x);
       RowExp<NV> row;
       row_exp<G, NV>(x, T, row);
-      const int at = place[v * ld_place + s];
-      float d = -kInf;
+      float l = -kInf;  // the place's logit
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (g * NV + j == at && at < a.n_res) d = row.z[j];
-      d = group_max<G>(d);
-      sum += (double)(row.sum != row.sum ? row.sum : row.empty || d == -kInf ? -kInf : d - logf(row.sum));
+      for (int j = 0; j < NV; ++j) l = g * NV + j == at ? x[j] : l;
+      l = group_max<G>(l);
+      sum += (double)(row.sum != row.sum ? row.sum : l == -kInf ? -kInf : row.z(l) - row.log_sum());
     }
   }
   if (g == 0) red[grp] = sum;
@@ -844,11 +870,11 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp_runs(PolicyArgs a, int
       load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + (v0 + grp) * a.ld_op, g * NV, R, x);
       RowExp<NV> row;
       row_exp<G, NV>(x, T, row);
-      const float ls = logf(row.sum);
+      const float ls = row.log_sum();
       float *t = table + grp * (R + 1);
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (g * NV + j < R) t[g * NV + j] = row.sum != row.sum ? row.sum : row.z[j] == -kInf ? -kInf : row.z[j] - ls;
+        if (g * NV + j < R) t[g * NV + j] = row.sum != row.sum ? row.sum : x[j] == -kInf ? -kInf : row.z(x[j]) - ls;
       if (g == 0) t[R] = row.sum != row.sum ? row.sum : -kInf;
     }
     __syncthreads();
@@ -1026,47 +1052,56 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
 
 // The gradient of a row from its softmax and what every resource received.
 template <int G, int NV>
-__device__ __forceinline__ void row_grad(const RowExp<NV> &row, float T, const float (&h)[NV], float (&out)[NV]) {
+__device__ __forceinline__ void row_grad(const RowExp<NV> &row, const float (&x)[NV], const float (&h)[NV], float (&out)[NV]) {
   float w = 0;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) w += row.z[j] == -kInf ? 0.0f : h[j];
+  for (int j = 0; j < NV; ++j) w += x[j] == -kInf ? 0.0f : h[j];
   w = group_sum<G>(w);
+  const float k = row.sum != row.sum ? row.sum : row.sum > 0 ? -w / row.sum * row.inv : 0.0f;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const float v = (h[j] - w * (row.e[j] / row.sum)) / T;
-    out[j] = row.sum != row.sum ? row.sum : row.z[j] == -kInf ? 0.0f : v;
-  }
+  for (int j = 0; j < NV; ++j) out[j] = k != k ? k : x[j] == -kInf ? 0.0f : __builtin_fmaf(row.e[j], k, h[j] * row.inv);
 }
 
-template <int G, int NV>
+// Few scenarios a row (ONE: at most one): a group of lanes takes them one after another.
+template <int G, int NV, bool ONE>
 __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t n_scen, const uint16_t *place,
                                                           int64_t ld_place, const float *weight, PolicyOut grad, Tile t) {
-  const int g = threadIdx.x % G, grp = threadIdx.x / G;
+  const int g = threadIdx.x % G, grp = threadIdx.x / G, r0 = g * NV;
   const int np = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
-  const int64_t pol_tiles = (a.n_pol + np - 1) / np;
-  const int64_t pol = blockIdx.x % pol_tiles * np + (grp & (np - 1));
-  const int64_t v0 = blockIdx.x / pol_tiles * (int64_t)nv * t.per + (grp >> t.log_pol);
-  if (pol >= a.n_pol) return;
+  const uint32_t pol_tiles = ((uint32_t)a.n_pol + np - 1) >> t.log_pol, v_tile = blockIdx.x / pol_tiles;
+  const uint32_t pol = ((blockIdx.x - v_tile * pol_tiles) << t.log_pol) + (grp & (np - 1));
+  const int64_t v0 = (int64_t)v_tile * nv * t.per + (grp >> t.log_pol);
+  if (pol >= (uint32_t)a.n_pol) return;
   const float T = policy_temperature(a, (int)pol);
-  for (int i = 0; i < t.per; ++i) {
-    const int64_t v = v0 + (int64_t)i * nv;
-    if (v >= a.n_ops) return;
+  uint64_t at_row = (uint64_t)pol * a.ld_pol + (uint64_t)v0 * a.ld_op, at_grad = (uint64_t)pol * grad.ld_pol + (uint64_t)v0 * grad.ld_op,
+           at_place = (uint64_t)v0 * ld_place;
+  const int64_t only = ONE ? only_scenario(a, pol, n_scen) : 0;
+  const float w_only = ONE && only < n_scen ? weight[only] : 0.0f;
+  const int steps = (int)min((int64_t)t.per, (a.n_ops - v0 + nv - 1) / nv);
+  for (int i = 0; i < steps; ++i, at_row += nv * a.ld_op, at_grad += nv * grad.ld_op, at_place += nv * ld_place) {
+    int at = -1;
+    if (ONE && only < n_scen) at = place[at_place + only] - r0;
     float x[NV], h[NV], out[NV];
-    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, g * NV, a.n_res, x);
+    load_row<NV>(a.logits, a.dtype, at_row, r0, a.n_res, x);
     RowExp<NV> row;
     row_exp<G, NV>(x, T, row);
+    if (ONE) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) h[j] = 0;
-    for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
-     for (int64_t s = beg; s < end; ++s) {
-      const int at = place[v * ld_place + s];
-      const float w = weight[s];
+      for (int j = 0; j < NV; ++j) h[j] = j == at ? w_only : 0.0f;
+    } else {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) h[j] += g * NV + j == at ? w : 0.0f;
-     }
-    });
-    row_grad<G, NV>(row, T, h, out);
-    store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g * NV, a.n_res, out);
+      for (int j = 0; j < NV; ++j) h[j] = 0;
+      for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
+        for (int64_t s = beg; s < end; ++s) {
+          const int to = place[at_place + s] - r0;
+          const float w = weight[s];
+#pragma unroll
+          for (int j = 0; j < NV; ++j) h[j] += j == to ? w : 0.0f;
+        }
+      });
+    }
+    row_grad<G, NV>(row, x, h, out);
+    store_row<NV>(grad.p, a.dtype, at_grad, r0, a.n_res, out);
   }
 }
 
@@ -1236,7 +1271,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
   float out[NV];
   RowExp<NV> row;
   row_exp<64, NV>(x, T, row);
-  row_grad<64, NV>(row, T, h, out);
+  row_grad<64, NV>(row, x, h, out);
   store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, R, out);
 }
 
@@ -1261,7 +1296,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, con
   for (int j = 0; j < NV; ++j) h[j] = (float)sum[j];
   RowExp<NV> row;
   row_exp<G, NV>(x, T, row);
-  row_grad<G, NV>(row, T, h, out);
+  row_grad<G, NV>(row, x, h, out);
   store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, out);
 }
 
@@ -1324,19 +1359,19 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
       }
     wave_order();
     float l = 0, out[NV];
-    const float ls = logf(row.sum);
+    const float ls = row.log_sum();
     const float wt = weight ? weight[row_id] : 1.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const float qj = any ? q[r0 + j] / sum : 0.0f;
-      if (qj > 0) l += qj * (logf(qj) - (row.z[j] - ls));
+      if (qj > 0) l += qj * (logf(qj) - (row.z(x[j]) - ls));
       const float pi = row.e[j] / row.sum;
       const float v1 = wt * (pi - qj) / T;
-      out[j] = row.z[j] == -kInf || !any ? 0.0f : v1;
+      out[j] = x[j] == -kInf || !any ? 0.0f : v1;
     }
     l = group_sum<G>(l);
     const float nan = row.sum + (any ? sum : 0.0f);
-    if (row.empty && any) l = kInf;
+    if (row.sum == 0 && any) l = kInf;  // an empty row
     if (nan != nan) l = nan;
     if (g == 0) loss[row_id] = l;
     if (grad.p) {
@@ -1595,7 +1630,10 @@ int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
   int64_t blocks;
   if (int rc = row_tile(a, t, blocks)) return rc;
   return by_row(a.n_res, [&](auto G, auto NV) {
-    k_policy_grad<G(), NV()><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t);
+    if (a.block == 1 && n_scen <= a.period)
+      k_policy_grad<G(), NV(), true><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t);
+    else
+      k_policy_grad<G(), NV(), false><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t);
     return launched();
   });
 }
