@@ -492,45 +492,47 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
     else
       merge_up<1, G>(s, g);
     const int k = top ? cut.k : cut.k - g * NV;  // so many of this lane's
-    const bool head = top || g == 0;             // element 0 is the first of the order
-    float cutoff = s[0];
+    float cutoff = -kInf;                        // the negative of the last kept
     uint32_t kept = 0;
     if (cut.p < 1) {
-      float ws[NV], mass = 0, before = 0, near = kInf;
+      // What lies behind the first k, or is -inf, adds nothing: the whole mass
+      // lies before it, so it is not kept.  Nothing lies before the first.
+      float off[NV], mass = 0, before = 0, near = kInf;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        ws[j] = mass;
+        off[j] = mass;
         mass += j < k ? weight(s[j]) : 0.0f;
       }
       if (!top) before = group_before<G>(mass, g, mass);
-      const float target = cut.p * mass;
+      before -= cut.p * mass;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const float off = ws[j] + before - target;
-        if (j > 0 || !head) near = fminf(near, j < k ? fabsf(off) : kInf);
-        const bool in = j < k && s[j] > -kInf && (off < 0 || (j == 0 && head));
-        cutoff = in ? s[j] : cutoff;
+        off[j] += before;
+        near = fminf(near, fabsf(off[j]));
+        const bool in = off[j] < 0;
+        cutoff = in ? -s[j] : cutoff;
         kept += in;
       }
       unsure |= near <= kMargin * mass;
     } else {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const bool in = j < k && s[j] > -kInf;
-        cutoff = in ? s[j] : cutoff;
-        kept += in;
+        cutoff = j < k ? -s[j] : cutoff;
+        kept += j < k;
       }
     }
-    cutoff = -group_max<G>(kept ? -cutoff : -kInf);
+    cutoff = -group_max<G>(cutoff);
     if (top && g) kept = 0;  // counted in lane 0
     // as many at or above it as are kept, or some of its equals are not
+    uint32_t above = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) kept += (x[j] >= cutoff ? 1u : 0u) << 16;
-    kept = group_sum<G>(kept);
-    if ((kept & 0xFFFFu) == kept >> 16) {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) w[j] = x[j] >= cutoff ? w[j] : 0.0f;
-    } else {
+    for (int j = 0; j < NV; ++j) {
+      const bool in = x[j] >= cutoff;
+      above += in;
+      if (!in) w[j] = 0;
+    }
+    kept = group_sum<G>(kept + (above << 16));
+    if ((kept & 0xFFFFu) != kept >> 16) {
       int ties = 0, all;
 #pragma unroll
       for (int j = 0; j < NV; ++j) ties += x[j] == cutoff;
@@ -539,7 +541,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const bool tie = x[j] == cutoff;
-        w[j] = x[j] > cutoff || (tie && rank < room) ? w[j] : 0.0f;
+        if (tie && rank >= room) w[j] = 0;
         rank += tie;
       }
     }
@@ -1429,11 +1431,13 @@ int launched() { return hipGetLastError() == hipSuccess ? SIM_OK : SIM_E_HIP; }
 
 constexpr int64_t kMaxBlocks = INT32_MAX;
 
-// Row kernels: up to 32 policies side by side (so that the scenarios of
-// neighbouring policies are written together), the other groups along the ops.
+// Row kernels: up to four policies (logp: scenarios) side by side, the other
+// groups along the ops, so that a wavefront's rows lie in few places.  1024 x
+// 6624 rows of 48 bf16, gradient and log-probabilities: 306 and 182 us with 4,
+// 315 and 183 with 8, 433 and 193 with 32, which would write 64 bytes of places together.
 int row_tile(const PolicyArgs &a, Tile &t, int64_t &blocks) {
   const int ng = kThreads / row_lanes(a.n_res);
-  t.log_pol = log2_at_least(a.n_pol, std::min(32, ng));
+  t.log_pol = log2_at_least(a.n_pol, std::min(4, ng));
   const int64_t np = 1 << t.log_pol, nv = ng >> t.log_pol, pol_tiles = (a.n_pol + np - 1) / np;
   t.per = (int)std::max<int64_t>(1, std::min<int64_t>(16, pol_tiles * ((a.n_ops + nv - 1) / nv) / 2048));
   blocks = pol_tiles * ((a.n_ops + nv * t.per - 1) / (nv * t.per));
@@ -1442,7 +1446,7 @@ int row_tile(const PolicyArgs &a, Tile &t, int64_t &blocks) {
 
 int64_t logp_tile(const PolicyArgs &a, int64_t n_scen, Tile &t, int64_t &blocks) {
   const int ng = kThreads / row_lanes(a.n_res);
-  t.log_pol = log2_at_least(n_scen, std::min(32, ng));
+  t.log_pol = log2_at_least(n_scen, std::min(4, ng));
   const int64_t ns = 1 << t.log_pol, nv = ng >> t.log_pol, tiles = (n_scen + ns - 1) / ns;
   const int64_t steps = (a.n_ops + nv - 1) / nv;
   t.per = (int)std::min<int64_t>(steps, std::max<int64_t>(4, steps * tiles / 4096));
