@@ -236,6 +236,33 @@ __device__ __forceinline__ void store_row(void *base, int32_t dtype, int64_t row
   }
 }
 
+// Rows whose order does not matter to the sums are held in pieces of V
+// resources, lane after lane, so that long rows are read in whole lines: lane g has
+// resource (j / V) G V + g V + j % V as its element j.
+constexpr int piece(int nv) { return nv > 8 ? 4 : nv; }
+
+template <int G, int NV>
+__device__ __forceinline__ void load_spread(const void *base, int32_t dtype, int64_t row, int g, int n, float (&x)[NV]) {
+  constexpr int V = piece(NV);
+#pragma unroll
+  for (int c = 0; c < NV / V; ++c) load_row<V>(base, dtype, row, (c * G + g) * V, n, reinterpret_cast<float (&)[V]>(x[c * V]));
+}
+
+template <int G, int NV>
+__device__ __forceinline__ void store_spread(void *base, int32_t dtype, int64_t row, int g, int n, const float (&x)[NV]) {
+  constexpr int V = piece(NV);
+#pragma unroll
+  for (int c = 0; c < NV / V; ++c) store_row<V>(base, dtype, row, (c * G + g) * V, n, reinterpret_cast<const float (&)[V]>(x[c * V]));
+}
+
+// Which element of lane g a resource is; negative: none.
+template <int G, int NV>
+__device__ __forceinline__ int spread_at(int r, int g) {
+  constexpr int V = piece(NV);
+  const int c = r / (G * V), in = r % (G * V);
+  return in / V == g ? c * V + in % V : -1;
+}
+
 // ---- settings, and which scenarios a policy has ----
 
 __device__ __forceinline__ float policy_temperature(const PolicyArgs &a, int p) {
@@ -361,7 +388,7 @@ __device__ __forceinline__ void merge_top(float (&v)[NV]) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) q[j] = __uint_as_float(lane_xor<2 * L - 1>(__float_as_uint(v[NV - 1 - j])));
 #pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = fmaxf(v[j], q[j]);
+    for (int j = 0; j < NV; ++j) v[j] = __builtin_amdgcn_fmed3f(v[j], q[j], kInf);
     merge_lane(v);
     merge_top<2 * L, G>(v);
   }
@@ -751,13 +778,13 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t 
     const int steps = (int)min((int64_t)t.per, (a.n_ops - v0 + nv - 1) / nv);
     for (int i = 0; i < steps; ++i, at_row += nv * a.ld_op, at_place += nv * ld_place) {
       float x[NV];
-      const int at = place[at_place];
-      load_row<NV>(a.logits, a.dtype, at_row, g * NV, a.n_res, x);
+      const int at = spread_at<G, NV>(place[at_place], g);
+      load_spread<G, NV>(a.logits, a.dtype, at_row, g, a.n_res, x);
       RowExp<NV> row;
       row_exp<G, NV>(x, T, row);
       float l = -kInf;  // the place's logit
 #pragma unroll
-      for (int j = 0; j < NV; ++j) l = g * NV + j == at ? x[j] : l;
+      for (int j = 0; j < NV; ++j) l = j == at ? x[j] : l;
       l = group_max<G>(l);
       sum += (double)(row.sum != row.sum ? row.sum : l == -kInf ? -kInf : row.z(l) - row.log_sum());
     }
@@ -1068,7 +1095,7 @@ __device__ __forceinline__ void row_grad(const RowExp<NV> &row, const float (&x)
 template <int G, int NV, bool ONE>
 __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t n_scen, const uint16_t *place,
                                                           int64_t ld_place, const float *weight, PolicyOut grad, Tile t) {
-  const int g = threadIdx.x % G, grp = threadIdx.x / G, r0 = g * NV;
+  const int g = threadIdx.x % G, grp = threadIdx.x / G;
   const int np = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
   const uint32_t pol_tiles = ((uint32_t)a.n_pol + np - 1) >> t.log_pol, v_tile = blockIdx.x / pol_tiles;
   const uint32_t pol = ((blockIdx.x - v_tile * pol_tiles) << t.log_pol) + (grp & (np - 1));
@@ -1082,9 +1109,9 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
   const int steps = (int)min((int64_t)t.per, (a.n_ops - v0 + nv - 1) / nv);
   for (int i = 0; i < steps; ++i, at_row += nv * a.ld_op, at_grad += nv * grad.ld_op, at_place += nv * ld_place) {
     int at = -1;
-    if (ONE && only < n_scen) at = place[at_place + only] - r0;
+    if (ONE && only < n_scen) at = spread_at<G, NV>(place[at_place + only], g);
     float x[NV], h[NV], out[NV];
-    load_row<NV>(a.logits, a.dtype, at_row, r0, a.n_res, x);
+    load_spread<G, NV>(a.logits, a.dtype, at_row, g, a.n_res, x);
     RowExp<NV> row;
     row_exp<G, NV>(x, T, row);
     if (ONE) {
@@ -1095,7 +1122,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
       for (int j = 0; j < NV; ++j) h[j] = 0;
       for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
         for (int64_t s = beg; s < end; ++s) {
-          const int to = place[at_place + s] - r0;
+          const int to = spread_at<G, NV>(place[at_place + s], g);
           const float w = weight[s];
 #pragma unroll
           for (int j = 0; j < NV; ++j) h[j] += j == to ? w : 0.0f;
@@ -1103,7 +1130,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
       });
     }
     row_grad<G, NV>(row, x, h, out);
-    store_row<NV>(grad.p, a.dtype, at_grad, r0, a.n_res, out);
+    store_spread<G, NV>(grad.p, a.dtype, at_grad, g, a.n_res, out);
   }
 }
 
@@ -1302,86 +1329,103 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, con
   store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, out);
 }
 
+// A group of lanes distils a row.  The teacher's entries are scattered over
+// the resources in LDS (q), so that the gradient is one pass over the row; the loss
+// is summed entry by entry.  An entry on a logit of -inf is not scattered: its
+// gradient is 0 and it makes the loss infinite.  Entries that share a resource are
+// found by writing every entry's number to its resource and reading it
+// back; one lane then adds them up in order.
 template <int G, int NV>
 __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, PolicyTop top, const float *weight,
                                                              float *loss, PolicyOut grad, int64_t rows) {
-  __shared__ float lds_q[kThreads * NV];
-  __shared__ uint32_t lds_first[kThreads * NV];
-  const int g = threadIdx.x % G, grp = threadIdx.x / G, r0 = g * NV;
+  constexpr int V = piece(NV), kWords = V % 4 == 0 ? 4 : 1;
+  __shared__ __align__(16) float lds_q[kThreads * NV];
+  __shared__ uint16_t lds_entry[kThreads * NV];
+  const int g = threadIdx.x % G, grp = threadIdx.x / G;
   float *q = lds_q + grp * (G * NV);
-  uint32_t *first = lds_first + grp * (G * NV);  // the entry that names a resource first
-  const int64_t n_groups = (int64_t)gridDim.x * (kThreads / G);
+  uint16_t *entry = lds_entry + grp * (G * NV);
+  const uint32_t n_groups = gridDim.x * (kThreads / G);
   for (int64_t row_id = (int64_t)blockIdx.x * (kThreads / G) + grp; row_id < rows; row_id += n_groups) {
-    const int64_t pol = row_id / a.n_ops, v = row_id - pol * a.n_ops;
+    const int64_t pol = (uint64_t)row_id < 1ull << 32 ? (uint32_t)row_id / (uint32_t)a.n_ops : row_id / a.n_ops, v = row_id - pol * a.n_ops;
     const float T = policy_temperature(a, (int)pol);
-    float x[NV];
-    load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, r0, a.n_res, x);
-    RowExp<NV> row;
-    row_exp<G, NV>(x, T, row);
+    const int64_t at_row = pol * a.ld_pol + v * a.ld_op;
     const uint16_t *ids = top.res + pol * top.ld_res_pol + v * top.ld_res_op;
-    const int64_t lrow = pol * top.ld_log_pol + v * top.ld_log_op;
+    const int64_t at_log = pol * top.ld_log_pol + v * top.ld_log_op;
+    float x[NV];
+    load_spread<G, NV>(a.logits, a.dtype, at_row, g, a.n_res, x);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) q[r0 + j] = 0, first[r0 + j] = 0xFFFFFFFFu;
-    float m = -kInf;
-    wave_order();
+    for (int j = 0; j < NV; j += kWords)
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) q[((j / V) * G + g) * V + j % V + i] = 0;
+    float m = -kInf;  // passes over NaN, which the sum then shows
     for (int k = g; k < top.top; k += G) {
       const int id = ids[k];
-      if (id >= a.n_res) continue;
-      const float y = load_elem(top.logits, a.dtype, lrow + k);
-      m = fmaxf(m, y);
-      if (y != -kInf) atomicMin(&first[id], (uint32_t)k);
+      const float y = load_elem(top.logits, a.dtype, at_log + k);
+      if (id < a.n_res && y != -kInf) {
+        m = fmaxf(m, y);
+        entry[id] = (uint16_t)k;
+      }
     }
     m = group_max<G>(m);
-    float sum = 0;
-    int again = 0, any = 0;
+    RowExp<NV> row;
+    row_exp<G, NV>(x, T, row);
+    const float ls = row.log_sum();
     wave_order();
+    float sum = 0;
+    uint32_t seen = 0;  // bit 0: an entry, bit 16: entries that share a resource
     for (int k = g; k < top.top; k += G) {
       const int id = ids[k];
-      if (id >= a.n_res) continue;
-      const float y = load_elem(top.logits, a.dtype, lrow + k);
-      if (y == -kInf) continue;
-      const float e = expf((y - m) / T);
+      const float y = load_elem(top.logits, a.dtype, at_log + k);
+      if (id >= a.n_res || y == -kInf) continue;
+      const float e = expf((y - m) * row.inv);
       sum += e;
-      any = 1;
-      if (first[id] == (uint32_t)k)
-        q[id] = e;
-      else
-        again = 1;
+      seen |= entry[id] == k ? 1u : 0x10001u;
+      if (load_elem(a.logits, a.dtype, at_row + id) > -kInf) q[id] = e;
     }
     sum = group_sum<G>(sum);
-    any = group_sum<G>(any);
-    again = group_sum<G>(again);
+    seen = group_sum<G>(seen);
     wave_order();
-    if (again && g == 0)  // a resource named twice: the later entries, in order
+    if (seen >> 16 && g == 0) {
+      for (int k = top.top - 1; k >= 0; --k) {
+        const int id = ids[k];
+        if (id >= a.n_res || load_elem(top.logits, a.dtype, at_log + k) == -kInf) continue;
+        entry[id] = (uint16_t)k;  // in the end the first one's
+        q[id] = 0;
+      }
       for (int k = 0; k < top.top; ++k) {
         const int id = ids[k];
         if (id >= a.n_res) continue;
-        const float y = load_elem(top.logits, a.dtype, lrow + k);
-        if (y != -kInf && first[id] != (uint32_t)k) q[id] += expf((y - m) / T);
+        const float y = load_elem(top.logits, a.dtype, at_log + k);
+        if (y != -kInf && load_elem(a.logits, a.dtype, at_row + id) > -kInf) q[id] += expf((y - m) * row.inv);
       }
+    }
     wave_order();
-    float l = 0, out[NV];
-    const float ls = row.log_sum();
-    const float wt = weight ? weight[row_id] : 1.0f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const float qj = any ? q[r0 + j] / sum : 0.0f;
-      if (qj > 0) l += qj * (logf(qj) - (row.z(x[j]) - ls));
-      const float pi = row.e[j] / row.sum;
-      const float v1 = wt * (pi - qj) / T;
-      out[j] = x[j] == -kInf || !any ? 0.0f : v1;
+    float l = 0;
+    const float inv = 1.0f / sum;
+    for (int k = g; k < top.top; k += G) {
+      const int id = ids[k];
+      const float y = load_elem(top.logits, a.dtype, at_log + k);
+      if (id >= a.n_res || y == -kInf || entry[id] != k) continue;
+      const float logit = load_elem(a.logits, a.dtype, at_row + id);
+      const float p = q[id] * inv;
+      if (!(logit > -kInf))
+        l = kInf;
+      else if (p > 0)
+        l += p * (logf(p) - (row.z(logit) - ls));
     }
     l = group_sum<G>(l);
-    const float nan = row.sum + (any ? sum : 0.0f);
-    if (row.sum == 0 && any) l = kInf;  // an empty row
-    if (nan != nan) l = nan;
-    if (g == 0) loss[row_id] = l;
+    const float nan = row.sum + (seen ? sum : 0.0f);  // NaN or not
+    if (g == 0) loss[row_id] = nan != nan ? nan : l;
     if (grad.p) {
-      if (nan != nan) {
+      const float w = (weight ? weight[row_id] : 1.0f) * row.inv;
+      const float ke = nan != nan ? nan : seen && row.sum > 0 ? w / row.sum : 0.0f, kq = seen ? -w * inv : 0.0f;
+      float out[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) out[j] = nan;
-      }
-      store_row<NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, r0, a.n_res, out);
+      for (int j = 0; j < NV; j += kWords)
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+          out[j + i] = __builtin_fmaf(row.e[j + i], ke, q[((j / V) * G + g) * V + j % V + i] * kq);
+      store_spread<G, NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g, a.n_res, out);
     }
     wave_order();
   }
