@@ -12,6 +12,7 @@ last device.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -48,6 +49,7 @@ GEN_SIGMA_UNIT = 2.0 * (2.0 * (65536.0**2 - 1.0) / 3.0) ** 0.5 / 2.0**40
 NO_PLACE = 65535
 
 _lib = None
+_HERE = contextlib.nullcontext()  # the device is the current one already
 
 
 class _PolicyStruct(ctypes.Structure):
@@ -397,18 +399,20 @@ class Policy:
             raise SimError(rc, "sim_policy")
 
     def _on(self, stream, *inputs):
-        """The stream of a call, and the context in which it allocates and
-        launches.  Inputs of other streams are kept until it has run."""
+        """The stream of a call (its handle), and the context in which it
+        allocates and launches.  Inputs of other streams are kept until it has
+        run."""
         import torch
-        cur = torch.cuda.current_stream(self.device)
-        if stream is None or stream == cur:
-            return cur, torch.cuda.device(self.device)
+        if stream is None:
+            raw = torch._C._cuda_getCurrentRawStream(self.device.index)
+            return raw, _HERE if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
         if stream.device != self.device:
             raise ValueError(f"stream is on {stream.device}, the logits on {self.device}")
-        for t in (self.logits, self.settings, *inputs):
-            if t is not None:
-                t.record_stream(stream)
-        return stream, torch.cuda.stream(stream)
+        if stream != torch.cuda.current_stream(self.device):
+            for t in (self.logits, self.settings, *inputs):
+                if t is not None:
+                    t.record_stream(stream)
+        return stream.cuda_stream, torch.cuda.stream(stream)
 
     def _place(self, place, what="place"):
         import torch
@@ -438,10 +442,12 @@ class Policy:
         with ctx:
             if out is None:
                 out = torch.empty((self.n_ops, S), dtype=torch.uint16, device=self.device)
-            optr, ldo, So = self._place(out, "out")
-            if So < S:
-                raise ValueError(f"out must hold {S} scenarios")
-            rc = _load().sim_policy_sample(self._c, S, uptr, ld, optr, ldo, st.cuda_stream)
+                optr, ldo = out.data_ptr(), S
+            else:
+                optr, ldo, So = self._place(out, "out")
+                if So < S:
+                    raise ValueError(f"out must hold {S} scenarios")
+            rc = _load().sim_policy_sample(self._c, S, uptr, ld, optr, ldo, st)
         if rc:
             raise SimError(rc, "sim_policy_sample")
         return out
@@ -460,7 +466,7 @@ class Policy:
                 raise ValueError(f"out must be float32 of shape ({S},) or longer, contiguous, on {self.device}")
             work, need = self._work(S)
             rc = _load().sim_policy_logp(self._c, S, pptr, ld, out.data_ptr(), work.data_ptr() if need else None,
-                                         need, st.cuda_stream)
+                                         need, st)
         if rc:
             raise SimError(rc, "sim_policy_logp")
         return out
@@ -481,7 +487,7 @@ class Policy:
             out, g = self._grad_out(out)
             work, need = self._work(S)
             rc = _load().sim_policy_grad(self._c, S, pptr, ld, weight.data_ptr(), *g,
-                                         work.data_ptr() if need else None, need, st.cuda_stream)
+                                         work.data_ptr() if need else None, need, st)
         if rc:
             raise SimError(rc, "sim_policy_grad")
         return out
@@ -490,6 +496,7 @@ class Policy:
         import torch
         if out is None:
             out = torch.empty(self.logits.shape, dtype=self.logits.dtype, device=self.device)
+            return out, (out.data_ptr(), self.n_ops * self.n_res, self.n_res)
         rows = out[None] if isinstance(out, torch.Tensor) and out.dim() == 2 else out
         return out, _dev_rows(rows, self.logits.dtype, (self.n_pol, self.n_ops, self.n_res), self.device, "grad")
 
@@ -520,7 +527,7 @@ class Policy:
             if want_grad:
                 grad, g = self._grad_out(grad)
             rc = _load().sim_policy_distill(self._c, *res, *log, K, None if weight is None else weight.data_ptr(),
-                                            loss.data_ptr(), *g, st.cuda_stream)
+                                            loss.data_ptr(), *g, st)
         if rc:
             raise SimError(rc, "sim_policy_distill")
         return loss, grad if want_grad else None

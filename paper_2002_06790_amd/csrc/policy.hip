@@ -815,21 +815,27 @@ __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
   return ~min_pair(~a, ~b);
 }
 
-// E consecutive places from p on, two a word as memory holds them; 65535
-// behind `have`.  `whole`: every lane of the wavefront has all eight, one
-// 16-byte load at any even address.  Nothing here reads what was loaded, so
-// several loads stay in flight.
-template <int E>
-__device__ __forceinline__ void load_places(const uint16_t *p, int have, bool whole, uint32_t (&w)[(E + 1) / 2]) {
-  if (E == 8 && whole) {
-    __builtin_memcpy(w, p, sizeof(w));
-  } else {
+// A lane's eight scenarios s .. s + 7 of [beg, end) are one load of 16 bytes, at
+// any even address.  A lane that has fewer takes the last eight instead and shares
+// some with the lane before; a lane that has none leaves its values as they
+// are.  Only a range of under eight is read one by one, 65535 (or 0)
+// behind its end.  Nothing here reads what was loaded, so several loads stay in flight.
+template <int E, class I>
+__device__ __forceinline__ I first_of(I s, I beg, I end) {
+  return end - beg >= E ? min(s, end - E) : s;
+}
+
+template <int E, class I>
+__device__ __forceinline__ void load_places(const uint16_t *p, I s, I beg, I end, uint32_t (&w)[(E + 1) / 2]) {
+  if (E == 8 && end - beg >= E) {
+    if (s < end) __builtin_memcpy(w, p + min(s, end - E), sizeof(w));
+    return;
+  }
 #pragma unroll
-    for (int i = 0; i < (E + 1) / 2; ++i) {
-      const uint32_t lo = 2 * i < have ? p[2 * i] : kNoPlace;
-      const uint32_t hi = 2 * i + 1 < have ? p[2 * i + 1] : kNoPlace;
-      w[i] = lo | hi << 16;
-    }
+  for (int i = 0; i < (E + 1) / 2; ++i) {
+    const uint32_t lo = s + 2 * i < end ? p[s + 2 * i] : kNoPlace;
+    const uint32_t hi = 2 * i + 1 < E && s + 2 * i + 1 < end ? p[s + 2 * i + 1] : kNoPlace;
+    w[i] = lo | hi << 16;
   }
 }
 
@@ -880,18 +886,16 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp_runs(PolicyArgs a, int
   const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - chunk * ps.n);
   if (pc.beg >= pc.end) return;
   const float T = policy_temperature(a, pc.pol);
-  const int64_t s0 = pc.beg + (int64_t)threadIdx.x * E;
-  const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - s0));
-  const bool whole = __all(have == E);
+  const int len = (int)(pc.end - pc.beg), s0 = threadIdx.x * E;
   const int v_end = (int)min((int64_t)a.n_ops, (chunk + 1) * (int64_t)ops_per);
   double total[E] = {};
   for (int v0 = (int)(chunk * (int64_t)ops_per); v0 < v_end; v0 += kRows) {
     const int rows = min(kRows, v_end - v0);
-    uint32_t at[kAhead][(E + 1) / 2];
+    uint32_t at[kAhead][(E + 1) / 2] = {};
     auto load = [&](int r) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
-        load_places<E>(place + (int64_t)(v0 + min(r + i, rows - 1)) * ld_place + s0, have, whole, at[i]);
+        load_places<E>(place + (int64_t)(v0 + min(r + i, rows - 1)) * ld_place + pc.beg, s0, 0, len, at[i]);
     };
     load(0);
     if (grp < rows) {
@@ -929,9 +933,11 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp_runs(PolicyArgs a, int
     }
     __syncthreads();
   }
+  float *to = part + chunk * n_scen + pc.beg + first_of<E>(s0, 0, len);
+  const int have = len >= E ? s0 < len ? E : 0 : len - s0;
 #pragma unroll
   for (int e = 0; e < E; ++e)
-    if (e < have) part[chunk * n_scen + s0 + e] = (float)total[e];
+    if (e < have) to[e] = (float)total[e];
 }
 
 constexpr int kJoinScen = 16;
@@ -966,29 +972,28 @@ __device__ __forceinline__ float border(double c, double total, double inv) {
   return (double)down * total >= c ? down : f;
 }
 
-// E consecutive random numbers; 0 behind `have`.
-template <int E>
-__device__ __forceinline__ void load_numbers(const float *p, int have, bool whole, float (&u)[E]) {
-  if (whole) {
-    __builtin_memcpy(u, p, sizeof(u));
+template <int E, class I>
+__device__ __forceinline__ void load_numbers(const float *p, I s, I beg, I end, float (&u)[E]) {
+  if (end - beg >= E) {
+    if (s < end) __builtin_memcpy(u, p + min(s, end - E), sizeof(u));
   } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) u[e] = e < have ? p[e] : 0.0f;
+    for (int e = 0; e < E; ++e) u[e] = s + e < end ? p[s + e] : 0.0f;
   }
 }
 
-template <int E>
-__device__ __forceinline__ void store_places(uint16_t *p, int have, bool whole, const uint32_t (&at)[E]) {
-  if (whole) {
+template <int E, class I>
+__device__ __forceinline__ void store_places(uint16_t *p, I s, I beg, I end, const uint32_t (&at)[E]) {
+  if (end - beg >= E) {
     typedef uint32_t words __attribute__((ext_vector_type(E / 2), aligned(2)));
     words w;
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) w[i] = at[2 * i] | at[2 * i + 1] << 16;
-    __builtin_nontemporal_store(w, (words *)p);
+    if (s < end) __builtin_nontemporal_store(w, (words *)(p + min(s, end - E)));
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      if (e < have) p[e] = (uint16_t)at[e];
+      if (s + e < end) p[s + e] = (uint16_t)at[e];
   }
 }
 
@@ -1017,15 +1022,12 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
   if (v >= a.n_ops) return;  // with WR > 1 a block has one row
   const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - vb * ps.n);
   if (pc.beg >= pc.end) return;
-  const float *pu = u + v * ld_u;
-  uint16_t *pp = place + v * ld_place;
-  int64_t s = pc.beg + (of_row * 64 + lane) * E;
-  float us[E];
-  auto load = [&] {
-    const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - s));
-    load_numbers<E>(pu + s, have, __all(have == E), us);
-  };
-  load();
+  const float *pu = u + v * ld_u + pc.beg;
+  uint16_t *pp = place + v * ld_place + pc.beg;
+  const int len = (int)(pc.end - pc.beg);
+  int s = (of_row * 64 + lane) * E;
+  float us[E] = {};
+  load_numbers<E>(pu, s, 0, len, us);
   if (of_row == 0) {
     float x[NV];
     load_row<NV>(a.logits, a.dtype, pc.pol * a.ld_pol + v * a.ld_op, lane * NV, a.n_res, x);
@@ -1047,7 +1049,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
   else
     wave_order();
   const bool ok = lds_ok[wave / WR];
-  while (s - lane * E < pc.end) {
+  while (s - lane * E < len) {
     uint32_t k[E];
     bool nan = !ok;
     float at[E], keep[E];
@@ -1058,9 +1060,9 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
       at[e] = __builtin_amdgcn_fmed3f(us[e], 0.0f, 2.0f);  // above 1 all are the same
       k[e] = 1;
     }
-    const int64_t now = s;
+    const int now = s;
     s += WR * 64 * E;
-    load();
+    load_numbers<E>(pu, s, 0, len, us);
     for (int l = 0; l < levels; ++l) {
       float t[E];
 #pragma unroll
@@ -1074,8 +1076,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
 #pragma unroll
       for (int e = 0; e < E; ++e) k[e] = ok && keep[e] == keep[e] ? k[e] : kNoPlace;
     }
-    const int have = (int)max((int64_t)0, min((int64_t)E, pc.end - now));
-    store_places<E>(pp + now, have, __all(have == E), k);
+    store_places<E>(pp, now, 0, len, k);
   }
 }
 
@@ -1212,14 +1213,12 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
   if (a.block >= 64 * E) {
     for_runs(a, (int)pol, from, to, [&](int64_t beg, int64_t end) {
       int64_t s = beg + t * E;
-      uint32_t w[RB][E / 2];
-      float y[E];
+      uint32_t w[RB][E / 2] = {};
+      float y[E] = {};
       auto load = [&] {
-        const int have = (int)max((int64_t)0, min((int64_t)E, end - s));
-        const bool whole = __all(have == E);
 #pragma unroll
-        for (int i = 0; i < RB; ++i) load_places<E>(pp + min(i, rows - 1) * ld_place + s, have, whole, w[i]);
-        load_numbers<E>(weight + s, have, whole, y);
+        for (int i = 0; i < RB; ++i) load_places<E>(pp + min(i, rows - 1) * ld_place, s, beg, end, w[i]);
+        load_numbers<E>(weight, s, beg, end, y);
       };
       load();
       while (s - t * E < end) {
@@ -1227,6 +1226,11 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
         double z[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) z[e] = (double)y[e] + magic - magic;
+        if (__any(s + E > end) && end - beg >= E) {  // what the lane before has, or nobody
+          const int not_mine = s < end ? (int)max((int64_t)0, s + E - end) : E;
+#pragma unroll
+          for (int e = 0; e < E; ++e) z[e] = e < not_mine ? 0.0 : z[e];
+        }
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
@@ -1530,15 +1534,15 @@ LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
   const int rows = kThreads / row_lanes(a.n_res);
   l.wide = std::min(a.block, n_scen) >= 8 * 64;
   l.pieces = make_pieces(a, n_scen, (int64_t)kThreads * (l.wide ? 8 : 1), l.ps);
-  // Whole tables of rows, and at most three blocks a CU, so that all run at
-  // once: 20000 ops of 64 resources in 16384 scenarios take 117 us with 720
-  // blocks (5.6 TB/s, what a plain read reaches), 127 with 632 and 138 with 1256,
-  // which leave some CUs a block more to do than others.
-  const int64_t tables = (a.n_ops + rows - 1) / rows, most = 768;
-  const int64_t want = std::max<int64_t>(1, std::min(tables, most / std::min(l.pieces, most)));
-  const int64_t per = (tables + want - 1) / want;
-  l.ops_per = (int)(per * rows);
-  l.chunks = (tables + per - 1) / per;
+  // At most three blocks a CU, so that all run at once (20000 ops of 64
+  // resources in 16384 scenarios take 117 us with 720 blocks, 5.6 TB/s, what a
+  // plain read reaches; 127 with 632 and 138 with 1256, which leave some CUs a block
+  // more to do than others), whole tables of rows or, for small batches, parts
+  // of one, down to 16 rows.
+  const int64_t most = 768, want = most / std::min(l.pieces, most);
+  const int64_t even = (a.n_ops + want - 1) / want, unit = even >= rows ? rows : std::min(16, rows);
+  l.ops_per = (int)((even + unit - 1) / unit * unit);
+  l.chunks = (a.n_ops + l.ops_per - 1) / l.ops_per;
   return l;
 }
 
@@ -1569,8 +1573,11 @@ int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, in
   const bool cut = a.settings || a.temperature == 0 || a.top_k >= 1 || a.top_p < 1 || a.min_p > 0;
   if (std::min(a.block, n_scen) >= kLongRun) {
     Pieces ps;
+    // Four wavefronts a row share one working-out of it, but wait for it: 20000
+    // rows of 64, 16384 scenarios, nothing cut: 334 us, and 369 with one; 79488 cut
+    // rows of 48, 4096 scenarios: 475 us, and 350 with one, whose wavefronts work out rows side by side.
     const int wr = !cut && std::min(a.block, n_scen) >= 2048 ? 4 : 1;
-    const int64_t pieces = make_pieces(a, n_scen, wr > 1 ? 8192 : 4096, ps), blocks = pieces * ((a.n_ops * (int64_t)wr + 3) / 4);
+    const int64_t pieces = make_pieces(a, n_scen, 4096, ps), blocks = pieces * ((a.n_ops * (int64_t)wr + 3) / 4);
     if (blocks > kMaxBlocks) return SIM_E_LIMIT;
     const int levels = log2_at_least(a.n_res, SIM_MAX_RES);
     return by_wave(a.n_res, [&](auto NV) {
