@@ -1361,31 +1361,37 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
     for (int j = 0; j < NV; j += kWords)
 #pragma unroll
       for (int i = 0; i < kWords; ++i) q[((j / V) * G + g) * V + j % V + i] = 0;
-    float m = -kInf;  // passes over NaN, which the sum then shows
-    for (int k = g; k < top.top; k += G) {
-      const int id = ids[k];
-      const float y = load_elem(top.logits, a.dtype, at_log + k);
-      if (id < a.n_res && y != -kInf) {
-        m = fmaxf(m, y);
-        entry[id] = (uint16_t)k;
+    // f(k, resource, teacher's logit, own logit) for this lane's entries; the first is kept
+    const int id0 = g < top.top ? ids[g] : kNoPlace;
+    const float y0 = g < top.top ? load_elem(top.logits, a.dtype, at_log + g) : -kInf;
+    const bool have0 = id0 < a.n_res && y0 != -kInf;
+    const float l0 = have0 ? load_elem(a.logits, a.dtype, at_row + id0) : -kInf;
+    auto entries = [&](auto f) {
+      if (have0) f(g, id0, y0, l0);
+      for (int k = g + G; k < top.top; k += G) {
+        const int id = ids[k];
+        const float y = load_elem(top.logits, a.dtype, at_log + k);
+        if (id < a.n_res && y != -kInf) f(k, id, y, load_elem(a.logits, a.dtype, at_row + id));
       }
-    }
+    };
+    float m = -kInf;  // passes over NaN, which the sum then shows
+    entries([&](int k, int id, float y, float) {
+      m = fmaxf(m, y);
+      entry[id] = (uint16_t)k;
+    });
     m = group_max<G>(m);
     RowExp<NV> row;
     row_exp<G, NV>(x, T, row);
     const float ls = row.log_sum();
     wave_order();
     float sum = 0;
-    uint32_t seen = 0;  // bit 0: an entry, bit 16: entries that share a resource
-    for (int k = g; k < top.top; k += G) {
-      const int id = ids[k];
-      const float y = load_elem(top.logits, a.dtype, at_log + k);
-      if (id >= a.n_res || y == -kInf) continue;
-      const float e = expf((y - m) * row.inv);
+    uint32_t seen = 0;  // low half: entries, high half: those that found another's number
+    entries([&](int k, int id, float y, float own) {
+      const float e = __builtin_amdgcn_exp2f((y - m) * row.inv * kLog2e);
       sum += e;
-      seen |= entry[id] == k ? 1u : 0x10001u;
-      if (load_elem(a.logits, a.dtype, at_row + id) > -kInf) q[id] = e;
-    }
+      seen += entry[id] == k ? 1u : 0x10001u;
+      if (own > -kInf) q[id] = e;
+    });
     sum = group_sum<G>(sum);
     seen = group_sum<G>(seen);
     wave_order();
@@ -1400,23 +1406,21 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
         const int id = ids[k];
         if (id >= a.n_res) continue;
         const float y = load_elem(top.logits, a.dtype, at_log + k);
-        if (y != -kInf && load_elem(a.logits, a.dtype, at_row + id) > -kInf) q[id] += expf((y - m) * row.inv);
+        if (y != -kInf && load_elem(a.logits, a.dtype, at_row + id) > -kInf)
+          q[id] += __builtin_amdgcn_exp2f((y - m) * row.inv * kLog2e);
       }
     }
     wave_order();
     float l = 0;
     const float inv = 1.0f / sum;
-    for (int k = g; k < top.top; k += G) {
-      const int id = ids[k];
-      const float y = load_elem(top.logits, a.dtype, at_log + k);
-      if (id >= a.n_res || y == -kInf || entry[id] != k) continue;
-      const float logit = load_elem(a.logits, a.dtype, at_row + id);
+    entries([&](int k, int id, float, float own) {
+      if (entry[id] != k) return;
       const float p = q[id] * inv;
-      if (!(logit > -kInf))
+      if (!(own > -kInf))
         l = kInf;
       else if (p > 0)
-        l += p * (logf(p) - (row.z(logit) - ls));
-    }
+        l += p * (kLn2 * __builtin_amdgcn_logf(p) - (row.z(own) - ls));
+    });
     l = group_sum<G>(l);
     const float nan = row.sum + (seen ? sum : 0.0f);  // NaN or not
     if (g == 0) loss[row_id] = nan != nan ? nan : l;
