@@ -439,7 +439,7 @@ int sim_static_run_generated(const sim_static *st, int64_t n_scen, const int32_t
  * is asynchronous on `stream`, allocates nothing and gives the same bits every
  * time.  Sums are held in at least 32 bits.
  */
-#define SIM_MAX_POLICY_SCEN (INT64_C(1) << 40)
+#define SIM_MAX_POLICY_SCEN (1 << 30)
 enum { SIM_F32 = 0, SIM_BF16 = 1, SIM_F16 = 2 };
 typedef struct sim_policy {
   const void *logits;

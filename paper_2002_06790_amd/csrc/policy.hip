@@ -788,7 +788,7 @@ __device__ __forceinline__ void row_weights(const float (&x)[NV], float m, float
   const float mc = m * c;
   const bool far = !(fabsf(mc) < 65536.0f);
   shift = 0;
-  if (__any(far)) {
+  if (far) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) e[j] = x[j] == -kInf ? 0.0f : __builtin_amdgcn_exp2f((x[j] - m) * c);  // inf - inf: NaN
   } else {
@@ -1586,11 +1586,15 @@ int64_t make_pieces(const PolicyArgs &a, int64_t n_scen, int64_t span, Pieces &p
   return runs * per_run;
 }
 
-// Whether scenarios share rows enough that a row's table is worth making: the
-// row kernels work through a whole row for every scenario.
-bool long_runs(const PolicyArgs &a, int64_t n_scen) { return std::min(a.block, n_scen) >= 4; }
+// Whether a row's table is worth making: the row kernel works through a whole
+// row for every scenario, two instructions a lane of its group; a table costs that
+// once, and 28 for a block of scenarios.
+bool long_runs(const PolicyArgs &a, int64_t n_scen) {
+  const int64_t lanes = row_lanes(a.n_res);
+  return std::min(a.block, n_scen) * lanes > lanes + 14;
+}
 
-constexpr int64_t kLongRun = 64;  // draws of a row
+constexpr double kPerUs = 600e3;  // wavefront instructions of all SIMDs in a microsecond
 
 // Whether the draws go row by row by groups of lanes, or a wavefront a row and
 // run: by the instructions of either, and by their latency where there are few
@@ -1601,10 +1605,21 @@ constexpr int64_t kLongRun = 64;  // draws of a row
 bool sample_by_rows(const PolicyArgs &a, int64_t n_scen) {
   const int64_t run = std::min(a.block, n_scen), lanes = row_lanes(a.n_res);
   const double rows = (double)a.n_pol * a.n_ops, rounds = (double)((std::max(n_scen / a.n_pol, run) + lanes - 1) / lanes);
-  const double us = 600e3;  // wavefront instructions of all SIMDs
+  const double us = kPerUs;
   const double groups = std::max(rows * lanes / 64 * (300 + 200 * rounds), rounds * 0.8 * us);
   const double waves = std::max((double)a.n_ops * n_scen / std::min<int64_t>(run, 4096) * 450 * std::max<int64_t>(1, lanes / 16), 6 * us);
-  return groups <= waves;
+  return groups <= waves || (double)a.n_ops * n_scen / run > 1e9;  // blocks of a launch
+}
+
+// Whether a gradient's scenarios are added by groups of lanes in registers (38
+// instructions each) or by a wavefront a row in LDS (about 480 a row, twice that for
+// the longest).  2000000 rows of 64: with 16, 32 and 63 scenarios a row 450, 658 and 1118 us
+// by groups, 1540 to 1664 by wavefronts; 127620 rows of 149 with 57: 233 us, and 111.
+bool grad_by_rows(const PolicyArgs &a, int64_t n_scen) {
+  const double lanes = row_lanes(a.n_res), rows = (double)a.n_pol * a.n_ops, long_row = a.n_res > 512 ? 2.3 : 1;
+  const double scen = (double)std::max(n_scen / a.n_pol, std::min(a.block, n_scen));
+  const double groups = std::max(rows * lanes / 64 * (250 * long_row + 38 * scen), scen * 0.2 * kPerUs);
+  return groups <= std::max(rows * 480 * long_row, 10 * kPerUs);
 }
 
 struct LogpRuns {
@@ -1624,7 +1639,7 @@ LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
   // plain read reaches; 127 with 632 and 138 with 1256, which leave some CUs a block
   // more to do than others), whole tables of rows or, for small batches, parts
   // of one, down to 16 rows.
-  const int64_t most = 768, want = most / std::min(l.pieces, most);
+  const int64_t most = l.wide ? 768 : 4096, want = most / std::min(l.pieces, most);
   const int64_t even = (a.n_ops + want - 1) / want, unit = even >= rows ? rows : std::min(16, rows);
   l.ops_per = (int)((even + unit - 1) / unit * unit);
   l.chunks = (a.n_ops + l.ops_per - 1) / l.ops_per;
@@ -1700,7 +1715,7 @@ int64_t policy_work(const PolicyArgs &a, int64_t n_scen) {
     int64_t blocks;
     logp = logp_tile(a, n_scen, t, blocks) * n_scen * 8;
   }
-  if (n_scen / a.n_pol >= kLongRun) {
+  if (!grad_by_rows(a, n_scen)) {
     const GradRuns r = grad_runs(a, n_scen);
     grad = kPeakBlocks * 4 + (r.splits > 1 ? r.splits * r.rows * a.n_res * 8 : 0);
   }
@@ -1742,7 +1757,7 @@ int launch_policy_logp(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
 
 int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *place, int64_t ld_place,
                        const float *weight, const PolicyOut &grad, void *work, hipStream_t st) {
-  if (n_scen / a.n_pol >= kLongRun) {
+  if (!grad_by_rows(a, n_scen)) {
     const GradRuns r = grad_runs(a, n_scen);
     if (r.rows * r.splits > kMaxBlocks) return SIM_E_LIMIT;
     float *peak = (float *)work;

@@ -11,6 +11,10 @@ HALF_STEP = {"float32": 2.0**-24, "bfloat16": 2.0**-8, "float16": 2.0**-11}
 #: below this a float16 is spaced evenly: half its step there
 HALF_TINY = {"float32": 0.0, "bfloat16": 0.0, "float16": 2.0**-25}
 NO_PLACE = 65535
+#: The smallest float32 that is held to EPS of itself is 2^-126.  A weight
+#: exp z below it may become 0, which moves it by less than 2^-126 and, as the
+#: weights' sum is 1 - 2^-8 at least, its probability by less than 2^-125.
+TINY = 2.0**-125
 
 
 def policy_of(s, block, scen0, n_pol):
@@ -125,7 +129,7 @@ def grad(logits, place, weight, settings, block=1, scen0=0, dtype="float32"):
             g[p, v] = np.where(allowed, (h - W * pi) / T, 0)
             d_w = EPS * ((n * A).sum() + 30 * np.abs(h).sum())
             d = EPS * n * A + pi * d_w + np.abs(W) * pi * EPS * (4 * np.abs(z) + 44)
-            d = (d + EPS * 2 * (np.abs(h) + np.abs(W) * pi)) / T + 4 * EPS * np.abs(g[p, v])
+            d = (d + EPS * 2 * (np.abs(h) + np.abs(W) * pi) + np.abs(W) * TINY) / T + 4 * EPS * np.abs(g[p, v])
             tol[p, v] = d + HALF_STEP[dtype] * (np.abs(g[p, v]) + d) + HALF_TINY[dtype]
     return g, tol
 
@@ -154,9 +158,9 @@ def distill(logits, ids, top, settings, weight=None, dtype="float32"):
             i = ids[p, v][use]
             q = np.bincount(i, t, R)[:R]
             # an entry's weight: the roundings of y, of the exponential, of a sum of K and of the quotient
-            dq = np.bincount(i, t * EPS * (4 * np.abs(y) + K + 40), R)[:R]
+            dq = np.bincount(i, t * EPS * (4 * np.abs(y) + K + 40) + TINY, R)[:R]
             pi = np.exp(lp)
-            dpi = pi * EPS * (4 * np.abs(z) + 44)
+            dpi = pi * EPS * (4 * np.abs(z) + 44) + TINY
             pos = q > 0
             if (pos & ~allowed).any():
                 loss[p, v] = np.inf

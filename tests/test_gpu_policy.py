@@ -79,6 +79,12 @@ SHAPES = [
     (3, 2, 1001, 1, 0, 3, "float32"),
     (1, 2, 1024, 600, 0, 600, "float16"),
     (4, 3, 12, 10**17, 3, 65, "float32"),  # one block longer than any scenario index: policy 0 alone
+    (3, 3, 12, 2**32, 2**32 - 20, 50, "float32"),  # policies change once, at an index beyond 32 bits
+    (3, 2, 70, 2**33, 3 * 2**33 * 5 - 30, 700, "bfloat16"),
+    (300, 11, 48, 1, 299, 300, "bfloat16"),  # one scenario each, the last policy first
+    (40, 13, 20, 7, 3, 275, "float16"),  # few scenarios each, the first and last policies fewer
+    (6, 9, 300, 40, 0, 233, "float32"),
+    (2, 300, 7, 90, 11, 180, "float32"),
 ]
 CUTS = [dict(), dict(temperature=0.7, top_k=3), dict(top_p=0.8), dict(min_p=0.1, temperature=1.5),
         dict(temperature=0.9, top_k=20, top_p=0.9, min_p=0.02), dict(temperature=0.0), dict(top_k=1), dict(top_p=0.0)]
@@ -164,6 +170,47 @@ def test_sample_far_apart_logits(mlsim):
     for cut in (dict(), dict(temperature=2.0), dict(top_k=3), dict(top_p=1 - 2.0**-24)):
         got = host16(mlsim.Policy(t, **cut).sample(torch.from_numpy(u).cuda()))
         assert np.array_equal(got, ref.sample(x, u.astype(np.float64), ref.settings_of(1, **cut))), cut
+
+
+@pytest.mark.parametrize("P,N,R,block,S", [(1, 3, 12, 1, 1), (1, 3, 70, 1, 6), (1, 2, 40, 1, 900), (9, 4, 33, 1, 9), (3, 2, 600, 2, 6), (1, 2, 600, 1, 700)])
+def test_logits_of_large_magnitude(mlsim, P, N, R, block, S):
+    """Logits around 10^6, where float32 holds them in steps of 1/16: only
+    differences count.  One row of ordinary ones among them."""
+    rng = np.random.default_rng(R)
+    x = (rng.choice([-1e6, 1e6], (P, N, 1)) + rng.normal(size=(P, N, R)) * 3).astype(np.float32)
+    x[0, 0] = rng.normal(size=R)
+    t = torch.from_numpy(x).cuda()
+    u = uniform(rng, N, S)
+    a = rng.integers(0, R, (N, S))
+    w = rng.normal(size=S).astype(np.float32)
+    x = x.astype(np.float64)
+    for cut in (dict(), dict(temperature=0.25, top_k=5, top_p=0.9), dict(temperature=3.0, min_p=0.1), dict(temperature=1e-30)):
+        print(f"large {P, N, R, block, S} {cut}", flush=True)
+        pol, st = mlsim.Policy(t, block=block, **cut), ref.settings_of(P, **cut)
+        got = host16(pol.sample(torch.from_numpy(u).cuda()))
+        assert np.array_equal(got, ref.sample(x, u.astype(np.float64), st, block)), cut
+        if cut.get("temperature", 1) > 1e-3:
+            ref.near(pol.logp(u16(a)).cpu().numpy(), *ref.logp(x, a, st, block), "logp")
+            g = pol.grad(u16(a), torch.from_numpy(w).cuda()).double().cpu().numpy()
+            ref.near(g, *ref.grad(x, a, w, st, block), "grad")
+
+
+def test_a_row_does_not_depend_on_its_neighbours(mlsim):
+    """The same bits for a row among others and alone."""
+    rng = np.random.default_rng(21)
+    N, R, S = 40, 30, 5
+    t, _ = make_logits(rng, 1, N, R, "float32")
+    t[0, 7] += 1e6  # another way of computing, for this row only
+    ids, y = u16(rng.integers(0, R, (1, N, 3))), torch.from_numpy(rng.normal(size=(1, N, 3))).float().cuda()
+    w = torch.from_numpy(rng.normal(size=S).astype(np.float32)).cuda()
+    place = u16(rng.integers(0, R, (N, S)))
+    grad = mlsim.Policy(t).grad(place, w)
+    loss, dgrad = mlsim.Policy(t).distill(ids, y)
+    for v in range(N):
+        one = mlsim.Policy(t[:, v:v + 1])
+        assert torch.equal(one.grad(place[v:v + 1], w), grad[:, v:v + 1])
+        l, g = one.distill(ids[:, v:v + 1], y[:, v:v + 1])
+        assert torch.equal(torch.nan_to_num(l), torch.nan_to_num(loss[:, v:v + 1])) and torch.equal(g, dgrad[:, v:v + 1])
 
 
 def draws(rng, x, S):
@@ -356,7 +403,8 @@ def test_offsets_beyond_32_bits(mlsim):
 def test_many_scenarios_of_one_row(mlsim):
     """A long batch over few ops, its counts odd: split over the scenarios."""
     rng = np.random.default_rng(13)
-    for P, N, R, block, S in ((1, 2, 5, 1, 300_001), (2, 1, 40, 100_000, 200_003), (1, 1, 700, 1, 70_001)):
+    for P, N, R, block, S in ((1, 2, 5, 1, 300_001), (2, 1, 40, 100_000, 200_003), (1, 1, 700, 1, 70_001),
+                              (3, 2, 20, 1, 30_001), (2, 1, 600, 3, 9_001), (4, 5, 64, 700, 20_011), (5, 9, 9, 2, 4_003)):
         print(f"many {P} {N} {R} {S}", flush=True)
         t, x = make_logits(rng, P, N, R, "float32")
         u = uniform(rng, N, S)
