@@ -58,9 +58,30 @@ __device__ __forceinline__ F group_all(F v, Op op) {
   return v;
 }
 
+// An infinity that the compiler does not know.  The median of two values and it is
+// the larger of the two (the other one where one is NaN) in one instruction; a
+// maximum, or a median with a known infinity, first clears signalling NaN in
+// each, which doubles a sort.
+__device__ __forceinline__ float some_infinity() {
+  float inf = kInf;
+  asm("" : "+v"(inf));
+  return inf;
+}
+
 template <int G>
 __device__ __forceinline__ float group_max(float v) {
-  return group_all<G>(v, [](float a, float b) { return fmaxf(a, b); });
+  const float inf = some_infinity();
+  return group_all<G>(v, [=](float a, float b) { return __builtin_amdgcn_fmed3f(a, b, inf); });
+}
+
+// The largest of a group's values, passing over NaN.
+template <int G, int NV>
+__device__ __forceinline__ float row_max(const float (&x)[NV]) {
+  const float inf = some_infinity();
+  float m = x[0];
+#pragma unroll
+  for (int j = 1; j < NV; ++j) m = __builtin_amdgcn_fmed3f(m, x[j], inf);
+  return group_max<G>(m);
 }
 template <int G, class F>
 __device__ __forceinline__ F group_sum(F v) {
@@ -384,13 +405,24 @@ __device__ __forceinline__ void sort_row(float (&v)[NV], int g) {
 template <int L, int G, int NV>
 __device__ __forceinline__ void merge_top(float (&v)[NV]) {
   if constexpr (L < G) {
-    float q[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) q[j] = __uint_as_float(lane_xor<2 * L - 1>(__float_as_uint(v[NV - 1 - j])));
-#pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = __builtin_amdgcn_fmed3f(v[j], q[j], kInf);
+    exchange<2 * L - 1, true>(v, some_infinity());
     merge_lane(v);
     merge_top<2 * L, G>(v);
+  }
+}
+
+// v[i], -inf from NV on: by the bits of i, one select for two elements.
+template <int S, int NV>
+__device__ __forceinline__ void pick_bits(float (&v)[NV], int i) {
+  if constexpr (S < NV) {
+    const bool odd = (i & S) != 0;
+#pragma unroll
+    for (int j = 0; j + S < NV; j += 2 * S) {
+      float r = v[j];
+      asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v[j]), "v"(v[j + S]), "s"(__ballot(odd)));
+      v[j] = r;
+    }
+    pick_bits<2 * S>(v, i);
   }
 }
 
@@ -493,10 +525,7 @@ struct RowNear {
 
 template <int G, int NV, bool CUT>
 __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, int g, RowNear<NV> &out) {
-  float m = x[0];
-#pragma unroll
-  for (int j = 1; j < NV; ++j) m = fmaxf(m, x[j]);
-  m = group_max<G>(m);
+  const float m = row_max<G>(x);
   const float c = kLog2e * (1.0f / cut.T), mc = m * c;
   bool unsure = !(fabsf(mc) < 65536.0f) && m > -kInf;
   auto weight = [&](float l) { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, c, -mc)); };
@@ -512,44 +541,57 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
 #pragma unroll
     for (int j = 0; j < NV; ++j) s[j] = x[j];
     // up to NV resources kept: every lane gets them all, from a shorter merge
-    const bool top = G > 1 && cut.k <= NV;
+    const bool top = G >= NV && cut.k <= NV;
     sort_lane<NV>(s);
     if (top)
       merge_top<1, G>(s);
     else
       merge_up<1, G>(s, g);
-    const int k = top ? cut.k : cut.k - g * NV;  // so many of this lane's
-    float cutoff = -kInf;                        // the negative of the last kept
+    float cutoff = -kInf;  // the negative of the last kept
     uint32_t kept = 0;
-    if (cut.p < 1) {
-      // What lies behind the first k, or is -inf, adds nothing: the whole mass
-      // lies before it, so it is not kept.  Nothing lies before the first.
-      float off[NV], mass = 0, before = 0, near = kInf;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        off[j] = mass;
-        mass += j < k ? weight(s[j]) : 0.0f;
+    // What lies behind the first k, or is -inf, adds nothing: the whole mass lies
+    // before it, so it is not kept.  Nothing lies before the first.
+    if (top) {
+      // lane g takes element g of the order
+      pick_bits<1>(s, g);
+      const float own = g < NV ? s[0] : -kInf;
+      bool in = g < cut.k;
+      if (cut.p < 1) {
+        float all;
+        const float off = group_before<G>(in ? weight(own) : 0.0f, g, all) - cut.p * all;
+        unsure |= fabsf(off) <= kMargin * all;
+        in = off < 0;
       }
-      if (!top) before = group_before<G>(mass, g, mass);
-      before -= cut.p * mass;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        off[j] += before;
-        near = fminf(near, fabsf(off[j]));
-        const bool in = off[j] < 0;
-        cutoff = in ? -s[j] : cutoff;
-        kept += in;
-      }
-      unsure |= near <= kMargin * mass;
+      cutoff = in ? -own : cutoff;
+      kept = in;
     } else {
+      const int k = cut.k - g * NV;  // so many of this lane's
+      if (cut.p < 1) {
+        float off[NV], mass = 0, near = kInf, all;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        cutoff = j < k ? -s[j] : cutoff;
-        kept += j < k;
+        for (int j = 0; j < NV; ++j) {
+          off[j] = mass;
+          mass += j < k ? weight(s[j]) : 0.0f;
+        }
+        const float before = group_before<G>(mass, g, all) - cut.p * all;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          off[j] += before;
+          near = fminf(near, fabsf(off[j]));
+          const bool in = off[j] < 0;
+          cutoff = in ? -s[j] : cutoff;
+          kept += in;
+        }
+        unsure |= near <= kMargin * all;
+      } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          cutoff = j < k ? -s[j] : cutoff;
+          kept += j < k;
+        }
       }
     }
     cutoff = -group_max<G>(cutoff);
-    if (top && g) kept = 0;  // counted in lane 0
     // as many at or above it as are kept, or some of its equals are not
     uint32_t above = 0;
 #pragma unroll
@@ -813,10 +855,7 @@ struct RowExp {
 
 template <int G, int NV>
 __device__ __forceinline__ void row_exp(const float (&x)[NV], float T, RowExp<NV> &o) {
-  o.m = x[0];
-#pragma unroll
-  for (int j = 1; j < NV; ++j) o.m = fmaxf(o.m, x[j]);
-  o.m = group_max<G>(o.m);
+  o.m = row_max<G>(x);
   o.inv = 1.0f / T;
   row_weights<NV>(x, o.m, o.inv * kLog2e, o.e, o.shift);
   float s = 0;
