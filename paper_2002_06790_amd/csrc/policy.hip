@@ -122,6 +122,19 @@ __device__ __forceinline__ T from_lane(T v, int lane) {
   return v;
 }
 
+// n += (a <= b), two instructions: a compare whose result is an addition's carry.
+__device__ __forceinline__ void count_le(uint32_t &n, float a, float b) {
+  asm("v_cmp_le_f32 vcc, %1, %2\n\tv_addc_co_u32 %0, vcc, 0, %0, vcc" : "+v"(n) : "v"(a), "v"(b) : "vcc");
+}
+
+// n += !(x < cutoff), and w = 0 where x < cutoff.
+__device__ __forceinline__ void keep_from(uint32_t &n, float &w, float x, float cutoff) {
+  asm("v_cmp_nlt_f32 vcc, %2, %3\n\tv_cndmask_b32 %1, 0, %1, vcc\n\tv_addc_co_u32 %0, vcc, 0, %0, vcc"
+      : "+v"(n), "+v"(w)
+      : "v"(x), "v"(cutoff)
+      : "vcc");
+}
+
 // v as the data-parallel move CTRL brings it to the rows of 16 lanes in ROWS, 0 elsewhere.
 template <int CTRL, int ROWS, class F>
 __device__ __forceinline__ F moved(F v) {
@@ -157,6 +170,8 @@ __device__ __forceinline__ F group_before(F v, int g, F &all) {
     all = moved<0xFF, 0xF>(in);  // quad 3 3 3 3
   else if constexpr (G == 64)
     all = from_lane(in, 63);
+  else if constexpr (sizeof(F) == 4)
+    all = group_sum<G>(v);  // as a float, another order of additions
   else
     all = __shfl(in, G - 1, G);
   F ex;
@@ -530,12 +545,9 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
   bool unsure = !(fabsf(mc) < 65536.0f) && m > -kInf;
   auto weight = [&](float l) { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, c, -mc)); };
   const float most = weight(m);  // 1 but for the rounding of mc, in every weight alike
-  float w[NV], nan = cut.ok ? 0.0f : __builtin_nanf("");  // a row of -inf: the weights are NaN
+  float w[NV];  // NaN in a row of -inf, and where a logit is NaN; no cut drops NaN, so the total shows it
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    w[j] = weight(x[j]);
-    if (CUT) nan += w[j];  // finite but for NaN; without a cut the sums show it
-  }
+  for (int j = 0; j < NV; ++j) w[j] = weight(x[j]);
   if (CUT && (cut.k < SIM_MAX_RES || cut.p < 1)) {
     float s[NV];
 #pragma unroll
@@ -595,11 +607,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
     // as many at or above it as are kept, or some of its equals are not
     uint32_t above = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const bool in = x[j] >= cutoff;
-      above += in;
-      if (!in) w[j] = 0;
-    }
+    for (int j = 0; j < NV; ++j) keep_from(above, w[j], x[j], cutoff);
     kept = group_sum<G>(kept + (above << 16));
     if ((kept & 0xFFFFu) != kept >> 16) {
       int ties = 0, all;
@@ -621,7 +629,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       near = fminf(near, fabsf(w[j] - least));
-      w[j] = w[j] < least ? 0.0f : w[j];
+      w[j] = w[j] < least ? 0.0f : w[j];  // NaN stays
     }
     unsure |= near <= 0x1p-15f * least;
   }
@@ -632,7 +640,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
     out.c[j] = sum;
   }
   out.before = group_before<G>(sum, g, out.total);
-  out.total += CUT ? group_sum<G>(nan - nan) : nan;
+  if (CUT && !cut.ok) out.total = __builtin_nanf("");
   out.unsure = unsure;
 }
 
@@ -718,8 +726,8 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, in
     uint32_t below = 0, upto = 0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      below += row.c[j] <= from;
-      upto += row.c[j] <= to;
+      count_le(below, row.c[j], from);
+      count_le(upto, row.c[j], to);
     }
     const uint32_t n = group_sum<G>(row.unsure + (below << 10) + (upto << 21));
     const bool drawn = act && (row.total > 0 || (n & 0x3FFu)) && now == now;
