@@ -352,8 +352,8 @@ class Policy:
     the global index of a call's first scenario.
 
     ``temperature``, ``top_k`` (0: all), ``top_p`` and ``min_p``: numbers, or
-    one per policy as a sequence or tensor (rounded to float32).  Only
-    ``sample`` reads the last three.
+    one per policy as a sequence or tensor (rounded to float32; tensors on the
+    GPU are copied on the current stream).  Only ``sample`` reads the last three.
 
     Calls run on ``stream`` (default: the current stream of the logits'
     device), are asynchronous and may be captured into a graph.  Gradients come
@@ -374,25 +374,29 @@ class Policy:
         if logits.dim() != 3:
             raise ValueError("logits must have shape (n_pol, n_ops, n_res) or (n_ops, n_res)")
         self.n_pol, self.n_ops, self.n_res = (int(x) for x in logits.shape)
+        if max(logits.shape) >= 2**31 or not all(-2**63 <= int(x) < 2**63 for x in (block, scen0)):
+            raise ValueError("more policies or ops than 2^31, or block or scen0 beyond 64 bits")
         if self.n_res > 1 and logits.stride(2) != 1:
             raise ValueError("logits must have unit stride along the resources")
         self.device = logits.device
         values = (temperature, top_k, top_p, min_p)
         self.settings = None
         if not all(isinstance(x, (int, float)) for x in values):
-            rows = []
-            for name, x in zip(("temperature", "top_k", "top_p", "min_p"), values):
-                x = torch.as_tensor(x, dtype=torch.float32).detach().to(self.device)
+            rows = [torch.as_tensor(x, dtype=torch.float32).detach() for x in values]
+            for name, x in zip(("temperature", "top_k", "top_p", "min_p"), rows):
                 if x.dim() > 1 or (x.dim() == 1 and x.numel() != self.n_pol):
                     raise ValueError(f"{name} must be a number or one per policy ({self.n_pol})")
-                rows.append(x.expand(self.n_pol))
-            self.settings = torch.stack(rows, 1).contiguous()
+            # host values are put together on the host: the copy is done when it returns, for any stream
+            where = self.device if any(x.is_cuda for x in rows) else torch.device("cpu")
+            rows = [x.to(where).expand(self.n_pol) for x in rows]
+            self.settings = torch.stack(rows, 1).contiguous().to(self.device)
             values = (1.0, 0, 1.0, 0.0)
         elif int(top_k) != top_k:
             raise ValueError("top_k must be a whole number")
+        top_k = max(-1, min(int(values[1]), 2**31 - 1))  # above n_res it is n_res
         self._c = _PolicyStruct(logits.data_ptr(), logits.stride(0), logits.stride(1), int(block), int(scen0),
                                 None if self.settings is None else self.settings.data_ptr(), values[0],
-                                int(values[1]), values[2], values[3], codes[logits.dtype], self.n_pol, self.n_ops,
+                                top_k, values[2], values[3], codes[logits.dtype], self.n_pol, self.n_ops,
                                 self.n_res)
         rc = _load().sim_policy_work(self._c, 1)  # checks the policy itself, on the host
         if rc < 0:
@@ -513,6 +517,8 @@ class Policy:
         if isinstance(top_logits, torch.Tensor) and top_logits.dim() == 2:
             top_logits = top_logits[None]
         K = int(top_res.shape[2]) if isinstance(top_res, torch.Tensor) and top_res.dim() == 3 else 0
+        if K >= 2**31:
+            raise ValueError(f"{K} entries a row")
         res = _dev_rows(top_res, torch.uint16, (self.n_pol, self.n_ops, K), self.device, "top_res")
         log = _dev_rows(top_logits, self.logits.dtype, (self.n_pol, self.n_ops, K), self.device, "top_logits")
         for t, what in ((weight, "weight"), (loss, "loss")):
@@ -643,11 +649,17 @@ class Graph:
         ``policy`` and the random numbers ``u`` (float32 [n_ops, S]) and replay
         them (sim_policy_sample, then as ``run``).  Returns ``(makespan, finish
         or None, status, place)``."""
+        import torch
         if policy.n_ops != self.n_ops or policy.n_res != self.n_res:
             raise ValueError(f"the policy is for {policy.n_ops} ops on {policy.n_res} resources, the graph has "
                              f"{self.n_ops} on {self.n_res}")
         if tuple(u.shape) != tuple(dur.shape):
             raise ValueError(f"u must have dur's shape {tuple(dur.shape)}")
+        _dev_matrix(dur, torch.int32, self.n_ops, "dur")
+        if dur.device != policy.device:
+            raise ValueError(f"dur is on {dur.device}, the policy on {policy.device}")
+        if stream is None:  # the draw and the replay on one
+            stream = torch.cuda.current_stream(policy.device)
         place = policy.sample(u, out=place, stream=stream)
         return (*self.run(dur, place=place, want_finish=want_finish, algo=algo, stream=stream, gap=gap,
                           delay=delay), place)

@@ -596,3 +596,51 @@ def test_python_refusals(mlsim):
     none = mlsim.Policy(t[:, :0])
     assert none.sample(u[:0]).shape == (0, 6) and (none.logp(place[:0]) == 0).all()
     assert none.grad(place[:0], w).shape == (2, 0, 3)
+
+
+def test_numbers_beyond_the_struct_s(mlsim):
+    """Numbers that do not fit the C struct are refused or mean what they say,
+    and are never cut off to their low bits."""
+    t = torch.randn((1, 4, 3), device="cuda")
+    for f in (lambda: mlsim.Policy(t.expand(2**32 + 1, 4, 3)), lambda: mlsim.Policy(t[:, :1].expand(1, 2**32 + 1, 3)),
+              lambda: mlsim.Policy(t, block=2**64 + 1), lambda: mlsim.Policy(t, scen0=2**64), lambda: mlsim.Policy(t, scen0=-2**64),
+              lambda: mlsim.Policy(t, top_k=-2**32)):
+        with pytest.raises((ValueError, mlsim.SimError)):
+            f()
+    u = torch.rand((4, 500), device="cuda")
+    all_kept = host16(mlsim.Policy(t).sample(u))
+    for top_k in (2**31, 2**32 + 1, 2.0**40):
+        assert np.array_equal(host16(mlsim.Policy(t, top_k=top_k).sample(u)), all_kept)
+
+
+def test_settings_of_each_kind(mlsim):
+    """Numbers, sequences, host and GPU tensors give the same draws, on a stream
+    that waits for nothing where the settings come from the host."""
+    rng = np.random.default_rng(8)
+    t, x = make_logits(rng, 3, 5, 12, "float32")
+    u = uniform(rng, 5, 60)
+    T, k, p = [0.5, 1.0, 2.0], [3, 0, 5], [0.9, 0.8, 1.0]
+    want = ref.sample(x, u.astype(np.float64), ref.settings_of(3, T, k, p, 0.01), 4)
+    ug, other = torch.from_numpy(u).cuda(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    kinds = [list, tuple, np.array, torch.tensor, lambda v: torch.tensor(v, device="cuda")]
+    for i, f in enumerate(kinds):
+        pol = mlsim.Policy(t, block=4, temperature=f(T), top_k=f(k), top_p=kinds[(i + 1) % 5](p), min_p=0.01)
+        if any(q is kinds[4] for q in (f, kinds[(i + 1) % 5])):
+            other.wait_stream(torch.cuda.current_stream())
+        got = pol.sample(ug, stream=other)
+        other.synchronize()
+        assert np.array_equal(host16(got), want), i
+
+
+def test_run_sampled_draws_nothing_for_bad_durations(mlsim):
+    w = W.make_config(1, n_scen=6)
+    g = mlsim.Graph.from_workload(w)
+    pol = mlsim.Policy(torch.zeros((w.n_ops, w.n_res), device="cuda"))
+    u = torch.rand((w.n_ops, 6), device="cuda")
+    place = u16(np.full((w.n_ops, 6), 7))
+    for dur in (torch.ones((w.n_ops, 6), dtype=torch.int64, device="cuda"), torch.ones((w.n_ops, 6), dtype=torch.int32)):
+        with pytest.raises((TypeError, ValueError)):
+            g.run_sampled(pol, dur, u, place=place)
+    assert (host16(place) == 7).all()
+    g.close()
