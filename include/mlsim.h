@@ -424,9 +424,10 @@ int sim_static_run_generated(const sim_static *st, int64_t n_scen, const int32_t
  *               (S / block) mod n_pol; block >= 1, scen0 >= 0.
  *   temperature, top_k, top_p, min_p   the settings of every policy, or
  *   settings    device float32 [n_pol][4]: those four for each policy (top_k
- *               as a number); the fields above are then not read.
- * Settings: a temperature T >= 0 (finite); top_k >= 0 (0: all); top_p and
- * min_p in [0, 1] (1 and 0: all).  Out of range, the fields return
+ *               as a number, its fraction dropped); the fields above are then
+ *               not read.
+ * Settings: a temperature T, 0 or a normal float32 (from 2^-126 on, finite);
+ * top_k >= 0 (0: all); top_p and min_p in [0, 1] (1 and 0: all).  Out of range, the fields return
  * SIM_E_INVAL; an entry of the device array makes its policy's rows invalid.
  * The struct is host memory, read during the call only.  At most
  * SIM_MAX_POLICY_SCEN scenarios a call.

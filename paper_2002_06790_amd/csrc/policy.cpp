@@ -29,7 +29,7 @@ int make_policy(const sim_policy *p, int64_t n_scen, PolicyArgs &a) {
   if (n_scen > SIM_MAX_POLICY_SCEN) return SIM_E_LIMIT;
   if (p->block < 1 || p->scen0 < 0 || n_scen > INT64_MAX - p->scen0) return SIM_E_INVAL;
   if (!p->settings) {
-    if (!(p->temperature >= 0) || !std::isfinite(p->temperature)) return SIM_E_INVAL;
+    if (p->temperature != 0 && !(p->temperature >= kLeastTemperature && std::isfinite(p->temperature))) return SIM_E_INVAL;
     if (p->top_k < 0 || !(p->top_p >= 0 && p->top_p <= 1) || !(p->min_p >= 0 && p->min_p <= 1)) return SIM_E_INVAL;
   } else if (!aligned(p->settings, 4)) {
     return SIM_E_INVAL;

@@ -303,6 +303,11 @@ __device__ __forceinline__ int spread_at(int r, int g) {
 
 // ---- settings, and which scenarios a policy has ----
 
+// A temperature is 0 or a normal float32: 1 / T and log2 e / T are finite then.
+__device__ __forceinline__ bool temperature_ok(float T) {
+  return T == 0 || (T >= kLeastTemperature && T < kInf);
+}
+
 __device__ __forceinline__ float policy_temperature(const PolicyArgs &a, int p) {
   return a.settings ? a.settings[(int64_t)p * 4] : a.temperature;
 }
@@ -321,7 +326,7 @@ __device__ __forceinline__ Cut policy_cut(const PolicyArgs &a, int p) {
     T = s[0], k = s[1], tp = s[2], mp = s[3];
   }
   Cut c;
-  c.ok = T >= 0 && T < kInf && k >= 0 && tp >= 0 && tp <= 1 && mp >= 0 && mp <= 1;
+  c.ok = temperature_ok(T) && k >= 0 && tp >= 0 && tp <= 1 && mp >= 0 && mp <= 1;
   c.k = k >= 1 ? (int)fminf(k, (float)SIM_MAX_RES) : SIM_MAX_RES;
   if (T == 0 || tp == 0) c.k = 1;
   c.T = T == 0 ? 1.0f : T;
@@ -875,7 +880,7 @@ __device__ __forceinline__ void row_exp(const float (&x)[NV], float T, RowExp<NV
 #pragma unroll
   for (int j = 0; j < NV; ++j) s += o.e[j];
   o.sum = group_sum<G>(s);
-  if (!(T > 0 && T < kInf)) o.sum = __builtin_nanf("");
+  if (T == 0 || !temperature_ok(T)) o.sum = __builtin_nanf("");
 }
 
 // Log-probabilities row by row: a group of lanes works through a scenario's
@@ -1212,9 +1217,9 @@ __device__ __forceinline__ void row_grad(const RowExp<NV> &row, const float (&x)
 #pragma unroll
   for (int j = 0; j < NV; ++j) w += x[j] == -kInf ? 0.0f : h[j];
   w = group_sum<G>(w);
-  const float k = row.sum != row.sum ? row.sum : row.sum > 0 ? -w / row.sum * row.inv : 0.0f;
+  const float k = row.sum != row.sum ? row.sum : row.sum > 0 ? -w / row.sum : 0.0f;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) out[j] = k != k ? k : x[j] == -kInf ? 0.0f : __builtin_fmaf(row.e[j], k, h[j] * row.inv);
+  for (int j = 0; j < NV; ++j) out[j] = k != k ? k : x[j] == -kInf ? 0.0f : __builtin_fmaf(row.e[j], k, h[j]) * row.inv;
 }
 
 // Few scenarios a row (ONE: at most one): a group of lanes takes them one after
@@ -1556,14 +1561,14 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
     const float nan = row.sum + (seen ? sum : 0.0f);  // NaN or not
     if (g == 0) loss[row_id] = nan != nan ? nan : l;
     if (grad.p) {
-      const float w = (weight ? weight[row_id] : 1.0f) * row.inv;
+      const float w = weight ? weight[row_id] : 1.0f;
       const float ke = nan != nan ? nan : seen && row.sum > 0 ? w / row.sum : 0.0f, kq = seen ? -w * inv : 0.0f;
       float out[NV];
 #pragma unroll
       for (int j = 0; j < NV; j += kWords)
 #pragma unroll
         for (int i = 0; i < kWords; ++i)
-          out[j + i] = __builtin_fmaf(row.e[j + i], ke, q[((j / V) * G + g) * V + j % V + i] * kq);
+          out[j + i] = __builtin_fmaf(row.e[j + i], ke, q[((j / V) * G + g) * V + j % V + i] * kq) * row.inv;
       store_spread<G, NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g, a.n_res, out);
     }
     wave_order();

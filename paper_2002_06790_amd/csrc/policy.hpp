@@ -9,6 +9,8 @@
 
 namespace mlsim {
 
+constexpr float kLeastTemperature = 0x1p-126f;
+
 // A policy's logits and settings (kernel argument; every field uniform).
 struct PolicyArgs {
   const void *logits;       // [n_pol][n_ops][n_res] of `dtype`, strides ld_pol and ld_op in elements

@@ -644,3 +644,27 @@ def test_run_sampled_draws_nothing_for_bad_durations(mlsim):
             g.run_sampled(pol, dur, u, place=place)
     assert (host16(place) == 7).all()
     g.close()
+
+
+@pytest.mark.parametrize("S", [3, 30, 3000])
+def test_the_least_temperature(mlsim, S):
+    """At T = 2^-126 a row's best resource has probability 1: its log-probability
+    is 0, and so is the gradient where it was taken, however large the weights;
+    a positive number below is no temperature."""
+    x = np.array([[[0.0, -1.0, -INF], [5.0, 4.0, 3.0], [-1.0, -3.0, -2.0], [-3e38, -INF, -INF]]] * 3)
+    t, u = torch.from_numpy(x).float().cuda(), torch.rand((4, S), device="cuda")
+    w = torch.full((S,), 1e30, device="cuda")
+    for T in (2.0**-126, [2.0**-126] * 3, [2.0**-127, 2.0**-126, 1e-45]):
+        pol = mlsim.Policy(t, temperature=T, block=S // 3)
+        bad = np.array([isinstance(T, list) and q < 2.0**-126 for q in (T if isinstance(T, list) else [T] * 3)])
+        place = pol.sample(u)
+        lost = bad[ref.policy_of(np.arange(S), S // 3, 0, 3)]
+        assert np.array_equal(host16(place), np.where(lost, ref.NO_PLACE, np.zeros((4, S)))), T
+        best = u16(np.zeros((4, S)))
+        logp = pol.logp(best).cpu().numpy()
+        assert np.isnan(logp[lost]).all() and (logp[~lost] == 0).all(), T
+        g = pol.grad(best, w).cpu().numpy()
+        assert np.isnan(g[bad]).all() and (g[~bad] == 0).all(), T
+        loss, dg = pol.distill(u16(np.zeros((3, 4, 1))), torch.zeros((3, 4, 1), device="cuda"), weight=torch.full((3, 4), 1e30, device="cuda"))
+        loss, dg = loss.cpu().numpy(), dg.cpu().numpy()
+        assert np.isnan(loss[bad]).all() and (loss[~bad] == 0).all() and np.isnan(dg[bad]).all() and (dg[~bad] == 0).all(), T

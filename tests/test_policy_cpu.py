@@ -148,3 +148,13 @@ def test_plain_gradients_agree_with_differences():
         assert abs((f[0] - f[1]) / 2e-5 - g[p, v, r]) < 1e-7
         f = [(dw * ref.distill(y, ids, top, st)[0]).sum() for y in (up, dn)]
         assert abs((f[0] - f[1]) / 2e-5 - dg[p, v, r]) < 1e-7
+
+
+def test_temperatures_and_numbers_of_scenarios(L):
+    """0 and normal float32 numbers are temperatures; up to 2^30 scenarios a call."""
+    for T in (0.0, 2.0**-126, 3e38):
+        assert L.sim_policy_work(struct(temperature=T), 8) >= 0
+    for T in (2.0**-127, 1e-45, -1e-45):
+        assert L.sim_policy_work(struct(temperature=T), 8) == mlsim.SIM_E_INVAL
+    assert L.sim_policy_work(struct(), 2**30) >= 0
+    assert L.sim_policy_work(struct(), 2**30 + 1) == mlsim.SIM_E_LIMIT
