@@ -375,17 +375,28 @@ __device__ __forceinline__ void merge_lanes(float (&v)[NV], int g) {
   if constexpr (S > 1) merge_lanes<S / 2>(v, g);
 }
 
+// Two rows' logits of 16 bits as whole numbers in the same order, which packed
+// instructions compare at once.
+typedef short key_pair __attribute__((ext_vector_type(2)));
+
+// The larger value first.
+__device__ __forceinline__ void put_in_order(float &a, float &b) {
+  const float hi = fmaxf(a, b), lo = fminf(a, b);
+  a = hi, b = lo;
+}
+__device__ __forceinline__ void put_in_order(key_pair &a, key_pair &b) {
+  const key_pair hi = __builtin_elementwise_max(a, b), lo = __builtin_elementwise_min(a, b);
+  a = hi, b = lo;
+}
+
 // A lane's bitonic values into falling order.
-template <int NV>
-__device__ __forceinline__ void merge_lane(float (&v)[NV]) {
+template <int NV, class F>
+__device__ __forceinline__ void merge_lane(F (&v)[NV]) {
 #pragma unroll
   for (int s = NV / 2; s >= 1; s /= 2)
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-      if (!(j & s)) {
-        const float hi = fmaxf(v[j], v[j + s]), lo = fminf(v[j], v[j + s]);
-        v[j] = hi, v[j + s] = lo;
-      }
+      if (!(j & s)) put_in_order(v[j], v[j + s]);
 }
 
 // Merge the sorted halves of 2 L lanes: the bitonic order, all steps the same way.
@@ -400,8 +411,8 @@ __device__ __forceinline__ void merge_up(float (&v)[NV], int g) {
 }
 
 // A lane's values in falling order: the odd-even merge exchanges.
-template <int NV>
-__device__ __forceinline__ void sort_lane(float (&v)[NV]) {
+template <int NV, class F>
+__device__ __forceinline__ void sort_lane(F (&v)[NV]) {
 #pragma unroll
   for (int p = 1; p < NV; p *= 2)
 #pragma unroll
@@ -410,10 +421,7 @@ __device__ __forceinline__ void sort_lane(float (&v)[NV]) {
       for (int j = k % p; j + k < NV; j += 2 * k)
 #pragma unroll
         for (int i = 0; i < k; ++i)
-          if (i + j + k < NV && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
-            const float hi = fmaxf(v[i + j], v[i + j + k]), lo = fminf(v[i + j], v[i + j + k]);
-            v[i + j] = hi, v[i + j + k] = lo;
-          }
+          if (i + j + k < NV && (i + j) / (2 * p) == (i + j + k) / (2 * p)) put_in_order(v[i + j], v[i + j + k]);
 }
 
 // Sort a group's G * NV values, the largest into element 0 of lane 0.
@@ -424,28 +432,59 @@ __device__ __forceinline__ void sort_row(float (&v)[NV], int g) {
 }
 
 // The NV largest of a group in falling order, in every lane, from the lanes' own.
-template <int L, int G, int NV>
-__device__ __forceinline__ void merge_top(float (&v)[NV]) {
+template <int X, int NV>
+__device__ __forceinline__ void take_larger(float (&v)[NV]) {
+  exchange<X, true>(v, some_infinity());
+}
+template <int X, int NV>
+__device__ __forceinline__ void take_larger(key_pair (&v)[NV]) {
+  key_pair q[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) q[j] = __builtin_bit_cast(key_pair, lane_xor<X>(__builtin_bit_cast(uint32_t, v[NV - 1 - j])));
+#pragma unroll
+  for (int j = 0; j < NV; ++j) v[j] = __builtin_elementwise_max(v[j], q[j]);
+}
+template <int L, int G, int NV, class F>
+__device__ __forceinline__ void merge_top(F (&v)[NV]) {
   if constexpr (L < G) {
-    exchange<2 * L - 1, true>(v, some_infinity());
+    take_larger<2 * L - 1>(v);
     merge_lane(v);
     merge_top<2 * L, G>(v);
   }
 }
 
 // v[i], -inf from NV on: by the bits of i, one select for two elements.
-template <int S, int NV>
-__device__ __forceinline__ void pick_bits(float (&v)[NV], int i) {
+template <int S, int NV, class F>
+__device__ __forceinline__ void pick_bits(F (&v)[NV], int i) {
   if constexpr (S < NV) {
     const bool odd = (i & S) != 0;
 #pragma unroll
     for (int j = 0; j + S < NV; j += 2 * S) {
-      float r = v[j];
+      F r = v[j];
       asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v[j]), "v"(v[j + S]), "s"(__ballot(odd)));
       v[j] = r;
     }
     pick_bits<2 * S>(v, i);
   }
+}
+
+// The NV largest of two rows of 16-bit logits (G >= NV lanes), the one of rank g
+// in lane g: numbers with the sign bit set are turned over, so that whole numbers
+// are in the floats' order (-0 before 0, which is the same logit).
+template <int G, int NV>
+__device__ __forceinline__ void top_of_two(const float (&x)[NV], const float (&y)[NV], bool f16, int g, float &own_x, float &own_y) {
+  auto turned = [](key_pair k) { return k ^ ((k >> (short)15) & (short)0x7FFF); };
+  key_pair v[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    v[j] = turned(f16 ? __builtin_bit_cast(key_pair, __builtin_amdgcn_cvt_pkrtz(x[j], y[j]))
+                      : __builtin_bit_cast(key_pair, __builtin_amdgcn_perm(__float_as_uint(y[j]), __float_as_uint(x[j]), 0x07060302u)));
+  sort_lane<NV>(v);
+  merge_top<1, G>(v);
+  pick_bits<1>(v, g);
+  const uint32_t own = __builtin_bit_cast(uint32_t, turned(v[0]));
+  own_x = g < NV ? half_value(own & 0xFFFFu, f16) : -kInf;
+  own_y = g < NV ? half_value(own >> 16, f16) : -kInf;
 }
 
 // Partial sums of a row's kept weights w = exp((l - max) / T), in 64 bits.
@@ -545,8 +584,15 @@ struct RowNear {
   bool unsure;   // of the group's lanes some may say so
 };
 
+template <int G, int NV>
+__device__ __forceinline__ bool keeps_few(const Cut &cut) {
+  return G >= NV && cut.k <= NV;
+}
+
+// `sorted`: own is element g of the order of the first NV, and the cut takes no more.
 template <int G, int NV, bool CUT>
-__device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, int g, RowNear<NV> &out) {
+__device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, int g, RowNear<NV> &out, bool sorted = false,
+                                         float own = 0) {
   const float m = row_max<G>(x);
   const float c = kLog2e * (1.0f / cut.T), mc = m * c;
   bool unsure = !(fabsf(mc) < 65536.0f) && m > -kInf;
@@ -557,23 +603,26 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
   for (int j = 0; j < NV; ++j) w[j] = weight(x[j]);
   if (CUT && (cut.k < SIM_MAX_RES || cut.p < 1)) {
     float s[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) s[j] = x[j];
     // up to NV resources kept: every lane gets them all, from a shorter merge
-    const bool top = G >= NV && cut.k <= NV;
-    sort_lane<NV>(s);
-    if (top)
-      merge_top<1, G>(s);
-    else
-      merge_up<1, G>(s, g);
+    const bool top = keeps_few<G, NV>(cut);
+    if (!sorted) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) s[j] = x[j];
+      sort_lane<NV>(s);
+      if (top) {
+        merge_top<1, G>(s);
+        pick_bits<1>(s, g);
+        own = g < NV ? s[0] : -kInf;
+      } else {
+        merge_up<1, G>(s, g);
+      }
+    }
     float cutoff = -kInf;  // the negative of the last kept
     uint32_t kept = 0;
     // What lies behind the first k, or is -inf, adds nothing: the whole mass lies
     // before it, so it is not kept.  Nothing lies before the first.
     if (top) {
       // lane g takes element g of the order
-      pick_bits<1>(s, g);
-      const float own = g < NV ? s[0] : -kInf;
       bool in = g < cut.k;
       if (cut.p < 1) {
         float all;
@@ -724,13 +773,13 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, in
   // unsigned: what is past the last op may wrap, and is not used
   uint64_t at_row = (uint64_t)walk.pol * a.ld_pol + (uint64_t)walk.v0 * a.ld_op, at_u = (uint64_t)walk.v0 * ld_u + s,
            at_place = (uint64_t)walk.v0 * ld_place + s;
-  for (int i = 0; __any(i < steps); ++i, at_row += walk.nv * a.ld_op, at_u += walk.nv * ld_u, at_place += walk.nv * ld_place) {
-    const bool act = i < steps;
-    const float now = act ? u[at_u] : 0.0f;
-    float x[NV];
+  auto load = [&](bool act, float (&x)[NV], float &now) {
+    now = act ? u[at_u] : 0.0f;
     load_row<NV>(a.logits, a.dtype, act ? (int64_t)at_row : 0, g * NV, a.n_res, x);
+  };
+  auto draw = [&](bool act, const float (&x)[NV], float now, bool sorted, float own) {
     RowNear<NV> row;
-    row_near<G, NV, CUT>(x, cut, g, row);
+    row_near<G, NV, CUT>(x, cut, g, row, sorted, own);
     // sure where as many sums lie below the target's margin as below its end, and not all
     const float margin = kMargin * row.total, mid = fmaxf(now, 0.0f) * row.total - row.before, from = mid - margin, to = mid + margin;
     uint32_t below = 0, upto = 0;
@@ -748,6 +797,33 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, in
       draw_sure<kWide>(a, from_lane(walk.pol, l), (int64_t)from_lane(at_row, l), u + from_lane(at_u, l),
                        place + from_lane(at_place, l), 0, 1, [](int) { return (int64_t)0; });
     }
+  };
+  auto next = [&] { at_row += walk.nv * a.ld_op, at_u += walk.nv * ld_u, at_place += walk.nv * ld_place; };
+  int i = 0;
+  if constexpr (CUT && G >= NV) {
+    // two rows at a time while every group has two that keep few
+    const bool f16 = a.dtype == SIM_F16;
+    if (a.dtype != SIM_F32 && __all(steps == 0 || keeps_few<G, NV>(cut))) {
+      for (; __any(i + 1 < steps); i += 2) {
+        float x[NV], y[NV], now_x, now_y, own_x, own_y;
+        const uint64_t at[3] = {at_row, at_u, at_place};
+        load(i < steps, x, now_x);
+        next();
+        load(i + 1 < steps, y, now_y);
+        top_of_two<G, NV>(x, y, f16, g, own_x, own_y);
+        const uint64_t then[3] = {at_row, at_u, at_place};
+        at_row = at[0], at_u = at[1], at_place = at[2];
+        draw(i < steps, x, now_x, true, own_x);
+        at_row = then[0], at_u = then[1], at_place = then[2];
+        draw(i + 1 < steps, y, now_y, true, own_y);
+        next();
+      }
+    }
+  }
+  for (; __any(i < steps); ++i, next()) {
+    float x[NV], now;
+    load(i < steps, x, now);
+    draw(i < steps, x, now, false, 0.0f);
   }
 }
 

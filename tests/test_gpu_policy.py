@@ -668,3 +668,37 @@ def test_the_least_temperature(mlsim, S):
         loss, dg = pol.distill(u16(np.zeros((3, 4, 1))), torch.zeros((3, 4, 1), device="cuda"), weight=torch.full((3, 4), 1e30, device="cuda"))
         loss, dg = loss.cpu().numpy(), dg.cpu().numpy()
         assert np.isnan(loss[bad]).all() and (loss[~bad] == 0).all() and np.isnan(dg[bad]).all() and (dg[~bad] == 0).all(), T
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("P,N,R,k", [(2048, 75, 48, 8), (1025, 260, 61, 5), (1024, 150, 100, 8), (4096, 67, 64, 1)])
+def test_many_rows_of_one_draw(mlsim, dtype, P, N, R, k):
+    """So many rows that a group takes several, with few kept: the same draws as
+    for a few policies at a time, and the plain form's.  Zeros of both signs,
+    subnormal numbers, ties, empty and invalid rows among them."""
+    rng = np.random.default_rng(R + k)
+    x = torch.from_numpy(rng.normal(size=(P, N, R)).astype(np.float32) * 2).to(TYPES[dtype])
+    x[::3, ::4] = torch.round(x[::3, ::4])
+    x[::7, 1] = torch.from_numpy(rng.choice([-1, -0.0, 0.0], (len(range(0, P, 7)), R)).astype(np.float32)).to(x.dtype)
+    tiny = torch.finfo(x.dtype).tiny
+    x[::5, 2] = (torch.from_numpy(rng.integers(-60, 60, (len(range(0, P, 5)), R))).double() * (tiny / 64)).to(x.dtype)
+    x[torch.from_numpy(rng.random((P, N, R)) < 0.1)] = -INF
+    x[3, 5] = -INF
+    x[4, 6, 7], x[5, 7, 8], x[6, 8, 9], x[7, 9, 10] = float("nan"), -float("nan"), INF, -INF
+    knobs = dict(temperature=np.full(P, 1.0, np.float32), top_k=rng.integers(1, k + 1, P).astype(np.float32),
+                 top_p=rng.choice([0.5, 0.9, 1.0], P).astype(np.float32), min_p=np.float32(0))
+    knobs["top_k"][100:200] = rng.integers(0, R, 100)  # others keep more
+    t, u = x.cuda(), uniform(rng, N, P)
+    ug = torch.from_numpy(u).cuda()
+    got = host16(mlsim.Policy(t, **knobs).sample(ug))
+    few = [host16(mlsim.Policy(t[a:a + 64], **{n: v if v.ndim == 0 else v[a:a + 64] for n, v in knobs.items()}).sample(ug[:, a:a + 64]))
+           for a in range(0, P, 64)]
+    assert np.array_equal(got, np.concatenate(few, 1))
+    st = ref.settings_of(P, **knobs)
+    for p in [*range(9), 100, 150, 199, *rng.integers(0, P, 10), P - 1]:
+        want = ref.sample(x[p:p + 1].double().numpy(), u[:, p:p + 1].astype(np.float64), st[p:p + 1])
+        assert np.array_equal(got[:, p:p + 1], want), p
+    one = dict(temperature=0.7, top_k=k, top_p=0.9)
+    got = host16(mlsim.Policy(t, **one).sample(ug))
+    few = [host16(mlsim.Policy(t[a:a + 64], **one).sample(ug[:, a:a + 64])) for a in range(0, P, 64)]
+    assert np.array_equal(got, np.concatenate(few, 1))
