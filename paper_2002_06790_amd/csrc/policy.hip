@@ -431,32 +431,38 @@ __device__ __forceinline__ void sort_row(float (&v)[NV], int g) {
   merge_up<1, G>(v, g);
 }
 
-// The NV largest of a group in falling order, in every lane, from the lanes' own.
-template <int X, int NV>
-__device__ __forceinline__ void take_larger(float (&v)[NV]) {
-  exchange<X, true>(v, some_infinity());
+// The larger of two values, or the smaller.
+__device__ __forceinline__ float larger(float a, float b, float inf) { return __builtin_amdgcn_fmed3f(a, b, inf); }
+__device__ __forceinline__ key_pair larger(key_pair a, key_pair b, float) { return __builtin_elementwise_max(a, b); }
+__device__ __forceinline__ float one_of(float a, float b, bool smaller, float inf) {
+  return __builtin_amdgcn_fmed3f(a, b, smaller ? -inf : inf);
 }
-template <int X, int NV>
-__device__ __forceinline__ void take_larger(key_pair (&v)[NV]) {
-  key_pair q[NV];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) q[j] = __builtin_bit_cast(key_pair, lane_xor<X>(__builtin_bit_cast(uint32_t, v[NV - 1 - j])));
-#pragma unroll
-  for (int j = 0; j < NV; ++j) v[j] = __builtin_elementwise_max(v[j], q[j]);
+__device__ __forceinline__ key_pair one_of(key_pair a, key_pair b, bool smaller, float) {
+  return smaller ? __builtin_elementwise_min(a, b) : __builtin_elementwise_max(a, b);
 }
+template <int X, class F>
+__device__ __forceinline__ F value_of(F v) {
+  return __builtin_bit_cast(F, lane_xor<X>(__builtin_bit_cast(uint32_t, v)));
+}
+
+// The NV largest of G lanes in falling order, in every lane, from the lanes' own.
 template <int L, int G, int NV, class F>
-__device__ __forceinline__ void merge_top(F (&v)[NV]) {
+__device__ __forceinline__ void merge_top(F (&v)[NV], float inf) {
   if constexpr (L < G) {
-    take_larger<2 * L - 1>(v);
+    F q[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) q[j] = value_of<2 * L - 1>(v[NV - 1 - j]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) v[j] = larger(v[j], q[j], inf);
     merge_lane(v);
-    merge_top<2 * L, G>(v);
+    merge_top<2 * L, G>(v, inf);
   }
 }
 
-// v[i], -inf from NV on: by the bits of i, one select for two elements.
-template <int S, int NV, class F>
+// v[j] = v[j + (i mod End)] for the j that End divides: a select for two elements.
+template <int S, int End, int NV, class F>
 __device__ __forceinline__ void pick_bits(F (&v)[NV], int i) {
-  if constexpr (S < NV) {
+  if constexpr (S < End) {
     const bool odd = (i & S) != 0;
 #pragma unroll
     for (int j = 0; j + S < NV; j += 2 * S) {
@@ -464,8 +470,32 @@ __device__ __forceinline__ void pick_bits(F (&v)[NV], int i) {
       asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v[j]), "v"(v[j + S]), "s"(__ballot(odd)));
       v[j] = r;
     }
-    pick_bits<2 * S>(v, i);
+    pick_bits<2 * S, End>(v, i);
   }
+}
+
+// A bitonic order of 2 S lanes, a value each, into falling order.
+template <int S, class F>
+__device__ __forceinline__ F merge_across(F v, int g, float inf) {
+  if constexpr (S == 0)
+    return v;
+  else
+    return merge_across<S / 2>(one_of(v, value_of<S>(v), (g & S) != 0, inf), g, inf);
+}
+
+// Value g in falling order of a group (G >= NV lanes, sorted each), for g < NV.  The
+// last merge is of two halves of the group, which hold their lists in every
+// lane: a lane takes two elements of it and goes on with one.
+template <int G, int NV, class F>
+__device__ __forceinline__ F top_value(F (&v)[NV], int g) {
+  const float inf = some_infinity();
+  constexpr int H = NV / 2;
+  merge_top<1, G / 2>(v, inf);
+  pick_bits<1, H>(v, g);
+  F a = v[0], b = v[H];
+  asm("s_nop 1" : "+v"(a), "+v"(b));  // between the selects and other lanes' reads of them
+  const F c = larger(a, value_of<G - 1>(b), inf), d = larger(b, value_of<G - 1>(a), inf);
+  return merge_across<H / 2>(one_of(c, d, (g & H) != 0, inf), g, inf);
 }
 
 // The NV largest of two rows of 16-bit logits (G >= NV lanes), the one of rank g
@@ -480,9 +510,7 @@ __device__ __forceinline__ void top_of_two(const float (&x)[NV], const float (&y
     v[j] = turned(f16 ? __builtin_bit_cast(key_pair, __builtin_amdgcn_cvt_pkrtz(x[j], y[j]))
                       : __builtin_bit_cast(key_pair, __builtin_amdgcn_perm(__float_as_uint(y[j]), __float_as_uint(x[j]), 0x07060302u)));
   sort_lane<NV>(v);
-  merge_top<1, G>(v);
-  pick_bits<1>(v, g);
-  const uint32_t own = __builtin_bit_cast(uint32_t, turned(v[0]));
+  const uint32_t own = __builtin_bit_cast(uint32_t, turned(top_value<G>(v, g)));
   own_x = g < NV ? half_value(own & 0xFFFFu, f16) : -kInf;
   own_y = g < NV ? half_value(own >> 16, f16) : -kInf;
 }
@@ -604,18 +632,17 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
   if (CUT && (cut.k < SIM_MAX_RES || cut.p < 1)) {
     float s[NV];
     // up to NV resources kept: every lane gets them all, from a shorter merge
-    const bool top = keeps_few<G, NV>(cut);
+    const bool top = sorted || keeps_few<G, NV>(cut);
     if (!sorted) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) s[j] = x[j];
       sort_lane<NV>(s);
-      if (top) {
-        merge_top<1, G>(s);
-        pick_bits<1>(s, g);
-        own = g < NV ? s[0] : -kInf;
-      } else {
-        merge_up<1, G>(s, g);
+      bool done = false;
+      if constexpr (G >= NV) {
+        if (top) own = top_value<G>(s, g), done = true;
+        own = g < NV ? own : -kInf;
       }
+      if (!done) merge_up<1, G>(s, g);
     }
     float cutoff = -kInf;  // the negative of the last kept
     uint32_t kept = 0;
