@@ -124,17 +124,41 @@ __device__ __forceinline__ T from_lane(T v, int lane) {
   return v;
 }
 
-// n += (a <= b), two instructions: a compare whose result is an addition's carry.
-__device__ __forceinline__ void count_le(uint32_t &n, float a, float b) {
-  asm("v_cmp_le_f32 vcc, %1, %2\n\tv_addc_co_u32 %0, vcc, 0, %0, vcc" : "+v"(n) : "v"(a), "v"(b) : "vcc");
+// A compare's result that is an addition's carry, or a select's, makes two or
+// three instructions an element where the compiler makes three or five.  A
+// vector instruction may read such a result two others after the compare, so
+// four elements take turns.
+
+// n += (a[0 .. 3] <= b)
+__device__ __forceinline__ void count_le(uint32_t &n, const float *a, float b) {
+  uint64_t p, q, r;
+  asm("v_cmp_le_f32 %1, %4, %8\n\tv_cmp_le_f32 %2, %5, %8\n\tv_cmp_le_f32 %3, %6, %8\n\t"
+      "v_addc_co_u32 %0, %1, 0, %0, %1\n\tv_cmp_le_f32 %1, %7, %8\n\t"
+      "v_addc_co_u32 %0, %2, 0, %0, %2\n\tv_addc_co_u32 %0, %3, 0, %0, %3\n\tv_addc_co_u32 %0, %1, 0, %0, %1"
+      : "+&v"(n), "=&s"(p), "=&s"(q), "=&s"(r)
+      : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b));
 }
 
-// n += !(x < cutoff), and w = 0 where x < cutoff.
-__device__ __forceinline__ void keep_from(uint32_t &n, float &w, float x, float cutoff) {
-  asm("v_cmp_nlt_f32 vcc, %2, %3\n\tv_cndmask_b32 %1, 0, %1, vcc\n\tv_addc_co_u32 %0, vcc, 0, %0, vcc"
-      : "+v"(n), "+v"(w)
-      : "v"(x), "v"(cutoff)
-      : "vcc");
+// n += !(x[0 .. 3] < cutoff), and w = 0 where x < cutoff.
+__device__ __forceinline__ void keep_from(uint32_t &n, float *w, const float *x, float cutoff) {
+  uint64_t p, q, r;
+  asm("v_cmp_nlt_f32 %5, %8, %12\n\tv_cmp_nlt_f32 %6, %9, %12\n\tv_cmp_nlt_f32 %7, %10, %12\n\t"
+      "v_cndmask_b32 %1, 0, %1, %5\n\tv_addc_co_u32 %0, %5, 0, %0, %5\n\tv_cmp_nlt_f32 %5, %11, %12\n\t"
+      "v_cndmask_b32 %2, 0, %2, %6\n\tv_addc_co_u32 %0, %6, 0, %0, %6\n\t"
+      "v_cndmask_b32 %3, 0, %3, %7\n\tv_addc_co_u32 %0, %7, 0, %0, %7\n\t"
+      "v_cndmask_b32 %4, 0, %4, %5\n\tv_addc_co_u32 %0, %5, 0, %0, %5"
+      : "+&v"(n), "+&v"(w[0]), "+&v"(w[1]), "+&v"(w[2]), "+&v"(w[3]), "=&s"(p), "=&s"(q), "=&s"(r)
+      : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(cutoff));
+}
+
+// k = 2 k + (u >= t), for four
+__device__ __forceinline__ void descend(uint32_t *k, const float *u, const float *t) {
+  uint64_t p, q, r;
+  asm("v_cmp_ge_f32 %4, %7, %11\n\tv_cmp_ge_f32 %5, %8, %12\n\tv_cmp_ge_f32 %6, %9, %13\n\t"
+      "v_addc_co_u32 %0, %4, %0, %0, %4\n\tv_cmp_ge_f32 %4, %10, %14\n\t"
+      "v_addc_co_u32 %1, %5, %1, %1, %5\n\tv_addc_co_u32 %2, %6, %2, %2, %6\n\tv_addc_co_u32 %3, %4, %3, %3, %4"
+      : "+&v"(k[0]), "+&v"(k[1]), "+&v"(k[2]), "+&v"(k[3]), "=&s"(p), "=&s"(q), "=&s"(r)
+      : "v"(u[0]), "v"(u[1]), "v"(u[2]), "v"(u[3]), "v"(t[0]), "v"(t[1]), "v"(t[2]), "v"(t[3]));
 }
 
 // v as the data-parallel move CTRL brings it to the rows of 16 lanes in ROWS, 0 elsewhere.
@@ -463,13 +487,9 @@ __device__ __forceinline__ void merge_top(F (&v)[NV], float inf) {
 template <int S, int End, int NV, class F>
 __device__ __forceinline__ void pick_bits(F (&v)[NV], int i) {
   if constexpr (S < End) {
-    const bool odd = (i & S) != 0;
+    const bool odd = __builtin_amdgcn_inverse_ballot_w64(__ballot((i & S) != 0));
 #pragma unroll
-    for (int j = 0; j + S < NV; j += 2 * S) {
-      F r = v[j];
-      asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(r) : "v"(v[j]), "v"(v[j + S]), "s"(__ballot(odd)));
-      v[j] = r;
-    }
+    for (int j = 0; j + S < NV; j += 2 * S) v[j] = odd ? v[j + S] : v[j];
     pick_bits<2 * S, End>(v, i);
   }
 }
@@ -492,8 +512,7 @@ __device__ __forceinline__ F top_value(F (&v)[NV], int g) {
   constexpr int H = NV / 2;
   merge_top<1, G / 2>(v, inf);
   pick_bits<1, H>(v, g);
-  F a = v[0], b = v[H];
-  asm("s_nop 1" : "+v"(a), "+v"(b));  // between the selects and other lanes' reads of them
+  const F a = v[0], b = v[H];
   const F c = larger(a, value_of<G - 1>(b), inf), d = larger(b, value_of<G - 1>(a), inf);
   return merge_across<H / 2>(one_of(c, d, (g & H) != 0, inf), g, inf);
 }
@@ -690,7 +709,7 @@ __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, i
     // as many at or above it as are kept, or some of its equals are not
     uint32_t above = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) keep_from(above, w[j], x[j], cutoff);
+    for (int j = 0; j < NV; j += 4) keep_from(above, w + j, x + j, cutoff);
     kept = group_sum<G>(kept + (above << 16));
     if ((kept & 0xFFFFu) != kept >> 16) {
       int ties = 0, all;
@@ -785,9 +804,9 @@ struct RowWalk {
 // draws.  A draw that lies within the roundings of a border (about one in a
 // thousand at 64 resources) is done again in 64 bits by the whole wavefront, so
 // that every answer is the 64-bit one.  Bound by vector instructions: 1024 x 6624
-// rows of 48 bf16 take 0.31 ms uncut and 0.54 ms with top_k 8 and top_p 0.9, of
-// which the sort of eight values a lane and the merges of the largest are a third
-// (with all sums in 64 bits and the cut searched bit by bit: 3.5 ms).
+// rows of 48 bf16 take 0.31 ms uncut and 0.453 ms with top_k 8 and top_p 0.9 (the
+// eight largest of two rows at once; 0.539 ms with a sort for each, 3.5 ms with all
+// sums in 64 bits and the cut searched bit by bit).
 template <int G, int NV, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
                                                                 uint16_t *place, int64_t ld_place, Tile t) {
@@ -811,9 +830,9 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, in
     const float margin = kMargin * row.total, mid = fmaxf(now, 0.0f) * row.total - row.before, from = mid - margin, to = mid + margin;
     uint32_t below = 0, upto = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      count_le(below, row.c[j], from);
-      count_le(upto, row.c[j], to);
+    for (int j = 0; j < NV; j += 4) {
+      count_le(below, row.c + j, from);
+      count_le(upto, row.c + j, to);
     }
     const uint32_t n = group_sum<G>(row.unsure + (below << 10) + (upto << 21));
     const bool drawn = act && (row.total > 0 || (n & 0x3FFu)) && now == now;
@@ -1228,12 +1247,6 @@ __device__ __forceinline__ void store_places(uint16_t *p, I s, I beg, I end, con
   }
 }
 
-// k = 2 k + (u >= t).  The compiler makes four instructions of this; a compare
-// whose result is the carry of an addition makes two.
-__device__ __forceinline__ void descend(uint32_t &k, float u, float t) {
-  asm("v_cmp_ge_f32 vcc, %1, %2\n\tv_addc_co_u32 %0, vcc, %0, %0, vcc" : "+v"(k) : "v"(u), "v"(t) : "vcc");
-}
-
 // WR wavefronts draw one row's placements for one piece.  The row's n_res - 1
 // borders go to LDS as float32, in the order of a binary tree's levels (node k
 // has 2k and 2k + 1 below it), so that a level's entries lie in consecutive
@@ -1301,7 +1314,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
 #pragma unroll
       for (int e = 0; e < E; ++e) t[e] = tree[k[e]];
 #pragma unroll
-      for (int e = 0; e < E; ++e) descend(k[e], at[e], t[e]);
+      for (int e = 0; e < E; e += 4) descend(k + e, at + e, t + e);
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) k[e] -= 1u << levels;
