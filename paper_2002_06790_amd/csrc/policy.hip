@@ -271,6 +271,25 @@ __device__ __forceinline__ void load_row(const void *base, int32_t dtype, int64_
   }
 }
 
+// The same as they stand in memory, of 16 bits, pair by pair.
+template <int NV>
+__device__ __forceinline__ void load_bits(const void *base, bool f16, int64_t row, int r0, int n, uint32_t (&w)[NV / 2]) {
+#pragma unroll
+  for (int i = 0; i < NV / 2; ++i) w[i] = f16 ? 0xFC00FC00u : 0xFF80FF80u;  // -inf
+  const uint16_t *p = (const uint16_t *)base + row + r0;
+  if (r0 + NV <= n) __builtin_memcpy(w, p, sizeof(w));
+  if (n % NV && r0 < n && r0 + NV > n) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (r0 + j < n) w[j / 2] = j % 2 ? (w[j / 2] & 0xFFFFu) | (uint32_t)p[j] << 16 : (w[j / 2] & 0xFFFF0000u) | p[j];
+  }
+}
+template <int NV>
+__device__ __forceinline__ void values_of(const uint32_t (&w)[NV / 2], bool f16, float (&x)[NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) x[j] = half_value(w[j / 2] >> 16 * (j % 2) & 0xFFFFu, f16);
+}
+
 template <int NV>
 __device__ __forceinline__ void store_row(void *base, int32_t dtype, int64_t row, int r0, int n, const float (&x)[NV]) {
   if (r0 >= n) return;
@@ -521,13 +540,13 @@ __device__ __forceinline__ F top_value(F (&v)[NV], int g) {
 // in lane g: numbers with the sign bit set are turned over, so that whole numbers
 // are in the floats' order (-0 before 0, which is the same logit).
 template <int G, int NV>
-__device__ __forceinline__ void top_of_two(const float (&x)[NV], const float (&y)[NV], bool f16, int g, float &own_x, float &own_y) {
+__device__ __forceinline__ void top_of_two(const uint32_t (&x)[NV / 2], const uint32_t (&y)[NV / 2], bool f16, int g, float &own_x,
+                                           float &own_y) {
   auto turned = [](key_pair k) { return k ^ ((k >> (short)15) & (short)0x7FFF); };
   key_pair v[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j)
-    v[j] = turned(f16 ? __builtin_bit_cast(key_pair, __builtin_amdgcn_cvt_pkrtz(x[j], y[j]))
-                      : __builtin_bit_cast(key_pair, __builtin_amdgcn_perm(__float_as_uint(y[j]), __float_as_uint(x[j]), 0x07060302u)));
+    v[j] = turned(__builtin_bit_cast(key_pair, __builtin_amdgcn_perm(y[j / 2], x[j / 2], j % 2 ? 0x07060302u : 0x05040100u)));
   sort_lane<NV>(v);
   const uint32_t own = __builtin_bit_cast(uint32_t, turned(top_value<G>(v, g)));
   own_x = g < NV ? half_value(own & 0xFFFFu, f16) : -kInf;
@@ -840,30 +859,50 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, in
     if (act && g == 0 && !redo) place[at_place] = drawn ? (uint16_t)(n >> 21) : kNoPlace;
     for (uint64_t left = __ballot(redo && g == 0); left; left &= left - 1) {
       const int l = __builtin_ctzll(left);
-      draw_sure<kWide>(a, from_lane(walk.pol, l), (int64_t)from_lane(at_row, l), u + from_lane(at_u, l),
+      draw_sure<kWide>(PolicyArgs(a), from_lane(walk.pol, l), (int64_t)from_lane(at_row, l), u + from_lane(at_u, l),
                        place + from_lane(at_place, l), 0, 1, [](int) { return (int64_t)0; });
     }
   };
   auto next = [&] { at_row += walk.nv * a.ld_op, at_u += walk.nv * ld_u, at_place += walk.nv * ld_place; };
   int i = 0;
   if constexpr (CUT && G >= NV) {
-    // two rows at a time while every group has two that keep few
-    const bool f16 = a.dtype == SIM_F16;
-    if (a.dtype != SIM_F32 && __all(steps == 0 || keeps_few<G, NV>(cut))) {
-      for (; __any(i + 1 < steps); i += 2) {
-        float x[NV], y[NV], now_x, now_y, own_x, own_y;
+    // two rows at a time while every group has two that keep few, the next two already loading
+    auto pairs = [&](auto type) {
+      constexpr bool f16 = type;
+      uint32_t w[2][NV / 2];
+      float now[2];
+      auto load_two = [&](int i) {
+        uint64_t row = at_row, of_u = at_u;
+#pragma unroll
+        for (int k = 0; k < 2; ++k, row += walk.nv * a.ld_op, of_u += walk.nv * ld_u) {
+          const bool act = i + k < steps;
+          now[k] = act ? u[of_u] : 0.0f;
+          load_bits<NV>(a.logits, f16, act ? (int64_t)row : 0, g * NV, a.n_res, w[k]);
+        }
+      };
+      load_two(0);
+      while (__any(i + 1 < steps)) {
+        float x[NV], y[NV], own_x, own_y;
+        const float now_x = now[0], now_y = now[1];
+        const bool act_x = i < steps, act_y = i + 1 < steps;
+        values_of<NV>(w[0], f16, x);
+        values_of<NV>(w[1], f16, y);
+        top_of_two<G, NV>(w[0], w[1], f16, g, own_x, own_y);
         const uint64_t at[3] = {at_row, at_u, at_place};
-        load(i < steps, x, now_x);
-        next();
-        load(i + 1 < steps, y, now_y);
-        top_of_two<G, NV>(x, y, f16, g, own_x, own_y);
+        next(), next();
+        i += 2;
+        load_two(i);
         const uint64_t then[3] = {at_row, at_u, at_place};
         at_row = at[0], at_u = at[1], at_place = at[2];
-        draw(i < steps, x, now_x, true, own_x);
-        at_row = then[0], at_u = then[1], at_place = then[2];
-        draw(i + 1 < steps, y, now_y, true, own_y);
+        draw(act_x, x, now_x, true, own_x);
         next();
+        draw(act_y, y, now_y, true, own_y);
+        at_row = then[0], at_u = then[1], at_place = then[2];
       }
+    };
+    if (__all(steps == 0 || keeps_few<G, NV>(cut))) {
+      if (a.dtype == SIM_F16) pairs(std::true_type{});
+      if (a.dtype == SIM_BF16) pairs(std::false_type{});
     }
   }
   for (; __any(i < steps); ++i, next()) {
@@ -947,13 +986,13 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_few(PolicyArgs a, in
       for (uint64_t left = __ballot(redo); left; left &= left - 1) {
         const int l = __builtin_ctzll(left);
         const int64_t rs = from_lane(at, l);
-        draw_sure<kWide>(a, from_lane(walk.pol, l), (int64_t)from_lane(at_row, l), u + from_lane(at_u, l), place + from_lane(at_place, l),
+        draw_sure<kWide>(PolicyArgs(a), from_lane(walk.pol, l), (int64_t)from_lane(at_row, l), u + from_lane(at_u, l), place + from_lane(at_place, l),
                          0, 1, [=](int) { return rs; });
       }
     }
     for (uint64_t left = __ballot(act && unsure && g == 0); left; left &= left - 1) {
       const int l = __builtin_ctzll(left), pol = from_lane(walk.pol, l);
-      draw_sure<kWide>(a, pol, (int64_t)from_lane(at_row, l), u + from_lane(at_u, l), place + from_lane(at_place, l), 0, INT32_MAX,
+      draw_sure<kWide>(PolicyArgs(a), pol, (int64_t)from_lane(at_row, l), u + from_lane(at_u, l), place + from_lane(at_place, l), 0, INT32_MAX,
                        PolicyScenarios(a, pol, n_scen));
     }
     wave_order();
