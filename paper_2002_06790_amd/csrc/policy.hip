@@ -346,6 +346,51 @@ __device__ __forceinline__ void store_spread(void *base, int32_t dtype, int64_t 
   for (int c = 0; c < NV / V; ++c) store_row<V>(base, dtype, row, (c * G + g) * V, n, reinterpret_cast<const float (&)[V]>(x[c * V]));
 }
 
+// A spread row as it stands in memory, for loads ahead of their use: what is
+// loaded is first looked at by values().
+template <int TYPE, int G, int NV>
+struct RowWords {
+  static constexpr int V = piece(NV), kPiece = TYPE == SIM_F32 ? V : V / 2;
+  uint32_t w[NV / V][kPiece];
+
+  __device__ __forceinline__ void load(const void *base, int64_t row, int g, int n) {
+#pragma unroll
+    for (int c = 0; c < NV / V; ++c) {
+      const int r0 = (c * G + g) * V;
+      if constexpr (TYPE == SIM_F32) {
+        const float *p = (const float *)base + row + r0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[c][j] = 0xFF800000u;  // -inf
+        if (r0 + V <= n) __builtin_memcpy(w[c], p, sizeof(w[c]));
+        if (n % V && r0 < n && r0 + V > n) {
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (r0 + j < n) w[c][j] = __float_as_uint(p[j]);
+        }
+      } else {
+        load_bits<V>(base, TYPE == SIM_F16, row, r0, n, w[c]);
+      }
+    }
+  }
+  __device__ __forceinline__ void values(float (&x)[NV]) const {
+#pragma unroll
+    for (int c = 0; c < NV / V; ++c) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        x[c * V + j] = TYPE == SIM_F32 ? __uint_as_float(w[c][j % kPiece])
+                                       : half_value(w[c][j / 2 % kPiece] >> 16 * (j % 2) & 0xFFFFu, TYPE == SIM_F16);
+    }
+  }
+};
+
+// f(the type) as a compile-time constant.
+template <class F>
+__device__ __forceinline__ void by_type(int32_t dtype, F f) {
+  if (dtype == SIM_F32) f(std::integral_constant<int, SIM_F32>{});
+  if (dtype == SIM_BF16) f(std::integral_constant<int, SIM_BF16>{});
+  if (dtype == SIM_F16) f(std::integral_constant<int, SIM_F16>{});
+}
+
 // Which element of lane g a resource is; negative: none.
 template <int G, int NV>
 __device__ __forceinline__ int spread_at(int r, int g) {
@@ -1074,18 +1119,25 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t 
     const int64_t v0 = chunk * nv * t.per + (grp >> t.log_pol);
     uint64_t at_row = (uint64_t)pol * a.ld_pol + (uint64_t)v0 * a.ld_op, at_place = (uint64_t)v0 * ld_place + s;
     const int steps = (int)min((int64_t)t.per, (a.n_ops - v0 + nv - 1) / nv);
-    for (int i = 0; i < steps; ++i, at_row += nv * a.ld_op, at_place += nv * ld_place) {
-      float x[NV];
-      const int at = spread_at<G, NV>(place[at_place], g);
-      load_spread<G, NV>(a.logits, a.dtype, at_row, g, a.n_res, x);
-      RowExp<NV> row;
-      row_exp<G, NV>(x, T, row);
-      float l = -kInf;  // the place's logit
+    by_type(a.dtype, [&](auto type) {
+      RowWords<type, G, NV> next;
+      int to = kNoPlace;
+      if (steps > 0) next.load(a.logits, at_row, g, a.n_res), to = place[at_place];
+      for (int i = 0; i < steps; ++i) {
+        float x[NV];
+        next.values(x);
+        const int at = spread_at<G, NV>(to, g);
+        at_row += nv * a.ld_op, at_place += nv * ld_place;
+        if (i + 1 < steps) next.load(a.logits, at_row, g, a.n_res), to = place[at_place];
+        RowExp<NV> row;
+        row_exp<G, NV>(x, T, row);
+        float l = -kInf;  // the place's logit
 #pragma unroll
-      for (int j = 0; j < NV; ++j) l = j == at ? x[j] : l;
-      l = group_max<G>(l);
-      sum += (double)(row.sum != row.sum ? row.sum : l == -kInf ? -kInf : row.z(l) - row.log_sum());
-    }
+        for (int j = 0; j < NV; ++j) l = j == at ? x[j] : l;
+        l = group_max<G>(l);
+        sum += (double)(row.sum != row.sum ? row.sum : l == -kInf ? -kInf : row.z(l) - row.log_sum());
+      }
+    });
   }
   if (g == 0) red[grp] = sum;
   __syncthreads();
@@ -1405,31 +1457,42 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
   const int64_t only = ONE ? only_scenario(a, pol, n_scen) : 0;
   const float w_only = ONE && only < n_scen ? weight[only] : 0.0f;
   const int steps = (int)min((int64_t)t.per, (a.n_ops - v0 + nv - 1) / nv);
-  for (int i = 0; i < steps; ++i, at_row += nv * a.ld_op, at_grad += nv * grad.ld_op, at_place += nv * ld_place) {
-    int at = -1;
-    if (ONE && only < n_scen) at = spread_at<G, NV>(place[at_place + only], g);
-    float x[NV], h[NV], out[NV];
-    load_spread<G, NV>(a.logits, a.dtype, at_row, g, a.n_res, x);
-    RowExp<NV> row;
-    row_exp<G, NV>(x, T, row);
-    if (ONE) {
+  by_type(a.dtype, [&](auto type) {
+    RowWords<type, G, NV> next;
+    int to = kNoPlace;
+    auto load = [&] {
+      next.load(a.logits, at_row, g, a.n_res);
+      if (ONE && only < n_scen) to = place[at_place + only];
+    };
+    if (steps > 0) load();
+    for (int i = 0; i < steps; ++i, at_grad += nv * grad.ld_op) {
+      float x[NV], h[NV], out[NV];
+      next.values(x);
+      const int at = ONE ? spread_at<G, NV>(to, g) : -1;
+      const uint64_t at_scen = at_place;
+      at_row += nv * a.ld_op, at_place += nv * ld_place;
+      if (i + 1 < steps) load();
+      RowExp<NV> row;
+      row_exp<G, NV>(x, T, row);
+      if (ONE) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) h[j] = j == at ? w_only : 0.0f;
-    } else {
+        for (int j = 0; j < NV; ++j) h[j] = j == at ? w_only : 0.0f;
+      } else {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) h[j] = 0;
-      for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
-        for (int64_t s = beg; s < end; ++s) {
-          const int to = spread_at<G, NV>(place[at_place + s], g);
-          const float w = weight[s];
+        for (int j = 0; j < NV; ++j) h[j] = 0;
+        for_runs(a, (int)pol, 0, n_scen, [&](int64_t beg, int64_t end) {
+          for (int64_t s = beg; s < end; ++s) {
+            const int mine = spread_at<G, NV>(place[at_scen + s], g);
+            const float w = weight[s];
 #pragma unroll
-          for (int j = 0; j < NV; ++j) h[j] += j == to ? w : 0.0f;
-        }
-      });
+            for (int j = 0; j < NV; ++j) h[j] += j == mine ? w : 0.0f;
+          }
+        });
+      }
+      row_grad<G, NV>(row, x, h, out);
+      store_spread<G, NV>(grad.p, type, at_grad, g, a.n_res, out);
     }
-    row_grad<G, NV>(row, x, h, out);
-    store_spread<G, NV>(grad.p, a.dtype, at_grad, g, a.n_res, out);
-  }
+  });
 }
 
 // The largest magnitude of the weights of each block's share (NaN counts as
