@@ -577,6 +577,20 @@ __device__ __forceinline__ F merge_across(F v, int g, float inf) {
     return merge_across<S / 2>(one_of(v, value_of<S>(v), (g & S) != 0, inf), g, inf);
 }
 
+// The element of a group's spread row that belongs to resource r: every lane picks
+// the one that its holder would, and takes the holder's.
+template <int G, int NV>
+__device__ __forceinline__ float spread_value(const float (&x)[NV], int r) {
+  constexpr int V = piece(NV);
+  float v[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) v[j] = x[j];
+  pick_bits<1, NV>(v, V == NV ? r : r / (G * V) * V + r % V);
+  if constexpr (G == 1) return v[0];
+  const int holder = (threadIdx.x & (64 - G)) + r / V % G;
+  return __uint_as_float(__builtin_amdgcn_ds_bpermute(holder * 4, __float_as_uint(v[0])));
+}
+
 // Value g in falling order of a group (G >= NV lanes, sorted each), for g < NV.  The
 // last merge is of two halves of the group, which hold their lists in every
 // lane: a lane takes two elements of it and goes on with one.
@@ -1126,15 +1140,13 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t 
       for (int i = 0; i < steps; ++i) {
         float x[NV];
         next.values(x);
-        const int at = spread_at<G, NV>(to, g);
+        const int to_now = to;
         at_row += nv * a.ld_op, at_place += nv * ld_place;
         if (i + 1 < steps) next.load(a.logits, at_row, g, a.n_res), to = place[at_place];
         RowExp<NV> row;
         row_exp<G, NV>(x, T, row);
-        float l = -kInf;  // the place's logit
-#pragma unroll
-        for (int j = 0; j < NV; ++j) l = j == at ? x[j] : l;
-        l = group_max<G>(l);
+        float l = spread_value<G, NV>(x, to_now);  // the place's logit
+        l = to_now < a.n_res ? l : -kInf;
         sum += (double)(row.sum != row.sum ? row.sum : l == -kInf ? -kInf : row.z(l) - row.log_sum());
       }
     });
