@@ -728,7 +728,7 @@ __device__ __forceinline__ bool keeps_few(const Cut &cut) {
 template <int G, int NV, bool CUT>
 __device__ __forceinline__ void row_near(const float (&x)[NV], const Cut &cut, int g, RowNear<NV> &out, bool sorted = false,
                                          float own = 0) {
-  const float m = row_max<G>(x);
+  const float m = sorted ? group_max<G>(own) : row_max<G>(x);
   const float c = kLog2e * (1.0f / cut.T), mc = m * c;
   bool unsure = !(fabsf(mc) < 65536.0f) && m > -kInf;
   auto weight = [&](float l) { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, c, -mc)); };
