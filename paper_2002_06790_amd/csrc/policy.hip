@@ -892,9 +892,9 @@ struct RowWalk {
 // draws.  A draw that lies within the roundings of a border (about one in a
 // thousand at 64 resources) is done again in 64 bits by the whole wavefront, so
 // that every answer is the 64-bit one.  Bound by vector instructions: 1024 x 6624
-// rows of 48 bf16 take 0.31 ms uncut and 0.453 ms with top_k 8 and top_p 0.9 (the
-// eight largest of two rows at once; 0.539 ms with a sort for each, 3.5 ms with all
-// sums in 64 bits and the cut searched bit by bit).
+// rows of 48 bf16 take 0.26 ms uncut and 0.41 ms with top_k 8 and top_p 0.9 (the
+// eight largest of two rows at once, the next two already loading; 0.54 ms with a
+// sort for each, 3.5 ms with all sums in 64 bits and the cut searched bit by bit).
 template <int G, int NV, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
                                                                 uint16_t *place, int64_t ld_place, Tile t) {
@@ -1114,9 +1114,10 @@ __device__ __forceinline__ void row_exp(const float (&x)[NV], float T, RowExp<NV
 }
 
 // Log-probabilities row by row: a group of lanes works through a scenario's
-// rows of a chunk of the ops.  Bound by vector instructions, two thirds of them
-// one unpacking, multiply-add, 2^x and addition an element: 1024 x 6624 rows of 48
-// bf16 take 179 us, 3.7 TB/s.
+// rows of a chunk of the ops, the next row loading meanwhile.  Memory and vector
+// instructions (two thirds of them one unpacking, multiply-add, 2^x and addition an
+// element) are even: 1024 x 6624 rows of 48 bf16 take 148 us, 4.5 TB/s (169
+// without the load ahead).
 template <int G, int NV>
 __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t n_scen, const uint16_t *place,
                                                           int64_t ld_place, double *part, Tile t) {
@@ -1452,8 +1453,8 @@ __device__ __forceinline__ void row_grad(const RowExp<NV> &row, const float (&x)
 }
 
 // Few scenarios a row (ONE: at most one): a group of lanes takes them one after
-// another.  Bound by memory: 1024 x 6624 rows of 48 bf16 take 309 us, 4.3 TB/s in
-// and out.
+// another, the next row loading meanwhile.  Bound by memory: 1024 x 6624 rows of
+// 48 bf16 take 273 us, 4.8 TB/s in and out (304 without the load ahead).
 template <int G, int NV, bool ONE>
 __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t n_scen, const uint16_t *place,
                                                           int64_t ld_place, const float *weight, PolicyOut grad, Tile t) {
@@ -1859,13 +1860,16 @@ int launched() { return hipGetLastError() == hipSuccess ? SIM_OK : SIM_E_HIP; }
 
 constexpr int64_t kMaxBlocks = INT32_MAX;
 
-// Row kernels: up to four policies (logp: scenarios) side by side, the other
-// groups along the ops, so that a wavefront's rows lie in few places.  1024 x
-// 6624 rows of 48 bf16, gradient and log-probabilities: 306 and 182 us with 4,
-// 315 and 183 with 8, 433 and 193 with 32, which would write 64 bytes of places together.
-int row_tile(const PolicyArgs &a, Tile &t, int64_t &blocks) {
+// Row kernels: up to `side` policies (logp: scenarios) side by side, the other
+// groups along the ops, so that a wavefront's rows lie in few places.  Draws of
+// short rows have 16 side by side, which write 32 bytes of places together, and
+// so have log-probabilities of the shortest, which read them.  With 4 and 16:
+// draws of 2048 x 6624 rows of 8 150 and 76 us, of 1024 x 6624 rows of 48 268 and
+// 261; log-probabilities of 4096 x 6624 rows of 8 148 and 113, of 1024 x 6624 rows
+// of 32 90 and 99; gradients of 1024 x 6624 rows of 32 185 and 218.
+int row_tile(const PolicyArgs &a, int side, Tile &t, int64_t &blocks) {
   const int ng = kThreads / row_lanes(a.n_res);
-  t.log_pol = log2_at_least(a.n_pol, std::min(4, ng));
+  t.log_pol = log2_at_least(a.n_pol, std::min(side, ng));
   const int64_t np = 1 << t.log_pol, nv = ng >> t.log_pol, pol_tiles = (a.n_pol + np - 1) / np;
   t.per = (int)std::max<int64_t>(1, std::min<int64_t>(16, pol_tiles * ((a.n_ops + nv - 1) / nv) / 2048));
   blocks = pol_tiles * ((a.n_ops + nv * t.per - 1) / (nv * t.per));
@@ -1874,7 +1878,7 @@ int row_tile(const PolicyArgs &a, Tile &t, int64_t &blocks) {
 
 int64_t logp_tile(const PolicyArgs &a, int64_t n_scen, Tile &t, int64_t &blocks) {
   const int ng = kThreads / row_lanes(a.n_res);
-  t.log_pol = log2_at_least(n_scen, std::min(4, ng));
+  t.log_pol = log2_at_least(n_scen, a.n_res <= 8 ? 16 : std::min(4, ng));
   const int64_t ns = 1 << t.log_pol, nv = ng >> t.log_pol, tiles = (n_scen + ns - 1) / ns;
   const int64_t steps = (a.n_ops + nv - 1) / nv;
   t.per = (int)std::min<int64_t>(steps, std::max<int64_t>(4, steps * tiles / 4096));
@@ -1897,11 +1901,12 @@ int64_t make_pieces(const PolicyArgs &a, int64_t n_scen, int64_t span, Pieces &p
 }
 
 // Whether a row's table is worth making: the row kernel works through a whole
-// row for every scenario, two instructions a lane of its group; a table costs that
-// once, and 28 for a block of scenarios.
+// row for every scenario, a table costs that twice and as much as 48 lanes more.
+// 1024 scenarios of 6624 rows of 48, 4 and 8 a table: 231 and 131 us, row by row
+// 138 and 134; 4096 of 8, 16 a table: 251 us, row by row 93.
 bool long_runs(const PolicyArgs &a, int64_t n_scen) {
   const int64_t lanes = row_lanes(a.n_res);
-  return std::min(a.block, n_scen) * lanes > lanes + 14;
+  return std::min(a.block, n_scen) * lanes > 2 * lanes + 48;
 }
 
 constexpr double kPerUs = 600e3;  // wavefront instructions of all SIMDs in a microsecond
@@ -2000,7 +2005,7 @@ int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, in
   }
   Tile t;
   int64_t blocks;
-  if (int rc = row_tile(a, t, blocks)) return rc;
+  if (int rc = row_tile(a, a.n_res <= 64 ? 16 : 4, t, blocks)) return rc;
   return by_row(a.n_res, [&](auto G, auto NV) {
     auto go = [&](auto cuts) {
       const dim3 grid((unsigned)blocks), block(kThreads);
@@ -2094,7 +2099,7 @@ int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
   }
   Tile t;
   int64_t blocks;
-  if (int rc = row_tile(a, t, blocks)) return rc;
+  if (int rc = row_tile(a, 4, t, blocks)) return rc;
   return by_row(a.n_res, [&](auto G, auto NV) {
     if (a.block == 1 && n_scen <= a.period)
       k_policy_grad<G(), NV(), true><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t);
