@@ -702,3 +702,22 @@ def test_many_rows_of_one_draw(mlsim, dtype, P, N, R, k):
     got = host16(mlsim.Policy(t, **one).sample(ug))
     few = [host16(mlsim.Policy(t[a:a + 64], **one).sample(ug[:, a:a + 64])) for a in range(0, P, 64)]
     assert np.array_equal(got, np.concatenate(few, 1))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("P,N,R", [(2048, 75, 48), (1025, 260, 61), (1024, 40, 600)])
+def test_many_rows_of_one_scenario(mlsim, dtype, P, N, R):
+    """So many rows that a group takes several: the gradient and the
+    log-probabilities have the same bits as for a few policies at a time."""
+    rng = np.random.default_rng(R)
+    t = (torch.randn((P, N, R), device="cuda") * 2).to(TYPES[dtype])
+    t[5, 3] = -INF
+    t[6, 4, 5] = float("nan")
+    a = u16(rng.integers(0, R + 1, (N, P)))
+    w = torch.randn(P, device="cuda")
+    g, l = mlsim.Policy(t).grad(a, w), mlsim.Policy(t).logp(a)
+    for p in range(0, P, 64):
+        some, place = mlsim.Policy(t[p:p + 64]), a.view(torch.int16)[:, p:p + 64].contiguous().view(torch.uint16)
+        assert torch.equal(torch.nan_to_num(g[p:p + 64]), torch.nan_to_num(some.grad(place, w[p:p + 64].contiguous())))
+        # summed in other chunks: to float32's step
+        assert torch.allclose(l[p:p + 64], some.logp(place), rtol=2.0**-22, atol=0, equal_nan=True)
