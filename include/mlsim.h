@@ -430,7 +430,8 @@ int sim_static_run_generated(const sim_static *st, int64_t n_scen, const int32_t
  * top_k >= 0 (0: all); top_p and min_p in [0, 1] (1 and 0: all).  Out of range, the fields return
  * SIM_E_INVAL; an entry of the device array makes its policy's rows invalid.
  * The struct is host memory, read during the call only.  At most
- * SIM_MAX_POLICY_SCEN scenarios a call.
+ * SIM_MAX_POLICY_SCEN scenarios a call; SIM_E_LIMIT also where a call would
+ * need more than 2^31 - 1 blocks of threads.
  *
  * With w_r = exp((l_r - max l) / T), the probability of resource r is
  * w_r / sum w.  A row (the logits of one op and policy) that holds NaN or +inf

@@ -876,11 +876,11 @@ struct RowWalk {
   int pol, np, nv, steps;  // steps of this group; 0 without a policy
   int64_t v0;
 
-  __device__ __forceinline__ RowWalk(const PolicyArgs &a, Tile t) {
+  __device__ __forceinline__ RowWalk(const PolicyArgs &a, Tile t, uint32_t block) {
     const int grp = threadIdx.x / G;
     np = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
-    const uint32_t pol_tiles = ((uint32_t)a.n_pol + np - 1) >> t.log_pol, v_tile = blockIdx.x / pol_tiles;
-    const uint32_t at = ((blockIdx.x - v_tile * pol_tiles) << t.log_pol) + (grp & (np - 1));
+    const uint32_t pol_tiles = ((uint32_t)a.n_pol + np - 1) >> t.log_pol, v_tile = block / pol_tiles;
+    const uint32_t at = ((block - v_tile * pol_tiles) << t.log_pol) + (grp & (np - 1));
     v0 = (int64_t)v_tile * nv * t.per + (grp >> t.log_pol);
     const bool live = at < (uint32_t)a.n_pol;
     pol = live ? (int)at : 0;
@@ -897,10 +897,11 @@ struct RowWalk {
 // sort for each, 3.5 ms with all sums in 64 bits and the cut searched bit by bit).
 template <int G, int NV, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
-                                                                uint16_t *place, int64_t ld_place, Tile t) {
+                                                                uint16_t *place, int64_t ld_place, Tile t,
+                                                                uint32_t first) {
   constexpr int kWide = G * NV > 64 ? G * NV / 64 : 1;
   const int g = threadIdx.x % G;
-  const RowWalk<G> walk(a, t);
+  const RowWalk<G> walk(a, t, first + blockIdx.x);
   const Cut cut = policy_cut(a, walk.pol);
   const int64_t s = only_scenario(a, walk.pol, n_scen);
   const int steps = s < n_scen ? walk.steps : 0;
@@ -1016,12 +1017,13 @@ struct PolicyScenarios {
 // 37 us.
 template <int G, int NV, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_few(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
-                                                                uint16_t *place, int64_t ld_place, Tile t) {
+                                                                uint16_t *place, int64_t ld_place, Tile t,
+                                                                uint32_t first) {
   constexpr int kWide = G * NV > 64 ? G * NV / 64 : 1, kRow = G * NV;
   __shared__ float lds[kThreads * NV];
   const int g = threadIdx.x % G;
   float *c = lds + threadIdx.x / G * kRow;
-  const RowWalk<G> walk(a, t);
+  const RowWalk<G> walk(a, t, first + blockIdx.x);
   const Cut cut = policy_cut(a, walk.pol);
   const PolicyScenarios scenario(a, walk.pol, n_scen);
   uint64_t at_row = (uint64_t)walk.pol * a.ld_pol + (uint64_t)walk.v0 * a.ld_op, at_u = (uint64_t)walk.v0 * ld_u,
@@ -1120,13 +1122,12 @@ __device__ __forceinline__ void row_exp(const float (&x)[NV], float T, RowExp<NV
 // without the load ahead).
 template <int G, int NV>
 __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t n_scen, const uint16_t *place,
-                                                          int64_t ld_place, double *part, Tile t) {
+                                                          int64_t ld_place, double *part, Tile t, uint32_t first) {
   __shared__ double red[kThreads / G];
   const int g = threadIdx.x % G, grp = threadIdx.x / G;
   const int ns = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
   const int64_t scen_tiles = (n_scen + ns - 1) / ns;
-  const int64_t s = blockIdx.x % scen_tiles * ns + (grp & (ns - 1));
-  const int64_t chunk = blockIdx.x / scen_tiles;
+  const int64_t block = first + blockIdx.x, chunk = block / scen_tiles, s0 = block % scen_tiles * ns, s = s0 + (grp & (ns - 1));
   double sum = 0;
   if (s < n_scen) {
     const int pol = policy_of(a, s);
@@ -1155,7 +1156,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_logp(PolicyArgs a, int64_t 
   if (g == 0) red[grp] = sum;
   __syncthreads();
   if (threadIdx.x < ns) {
-    const int64_t so = blockIdx.x % scen_tiles * ns + threadIdx.x;
+    const int64_t so = s0 + threadIdx.x;
     double all = 0;
     for (int i = 0; i < nv; ++i) all += red[(i << t.log_pol) + threadIdx.x];
     if (so < n_scen) part[chunk * n_scen + so] = all;
@@ -1241,13 +1242,14 @@ __device__ __forceinline__ Piece piece_of(const PolicyArgs &a, const Pieces &ps,
 // at logp_runs).
 template <int G, int NV, int E>
 __global__ __launch_bounds__(kThreads) void k_policy_logp_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
-                                                               int64_t ld_place, float *part, Pieces ps, int ops_per) {
+                                                               int64_t ld_place, float *part, Pieces ps, int ops_per,
+                                                               uint32_t first) {
   constexpr int kRows = kThreads / G;  // rows of one table
   constexpr int kAhead = 4;            // rows whose places are loaded together
   __shared__ float table[kRows * (G * NV + 1)];
   const int g = threadIdx.x % G, grp = threadIdx.x / G, R = a.n_res;
-  const uint32_t chunk = blockIdx.x / ps.n;
-  const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - chunk * ps.n);
+  const uint32_t block = first + blockIdx.x, chunk = block / ps.n;
+  const Piece pc = piece_of(a, ps, n_scen, block - chunk * ps.n);
   if (pc.beg >= pc.end) return;
   const float T = policy_temperature(a, pc.pol);
   const int len = (int)(pc.end - pc.beg), s0 = threadIdx.x * E;
@@ -1308,10 +1310,10 @@ constexpr int kJoinScen = 16;
 
 // The chunks' sums joined in order: sixteen lanes a scenario.
 template <class F>
-__global__ __launch_bounds__(kThreads) void k_policy_join(const F *part, int64_t chunks, int64_t n_scen, float *logp) {
+__global__ __launch_bounds__(kThreads) void k_policy_join(const F *part, int64_t chunks, int64_t n_scen, float *logp, uint32_t first) {
   constexpr int kScen = kJoinScen, kLanes = kThreads / kScen;
   __shared__ double red[kLanes][kScen];
-  const int64_t s = (int64_t)blockIdx.x * kScen + threadIdx.x % kScen;
+  const int64_t s = (int64_t)(first + blockIdx.x) * kScen + threadIdx.x % kScen;
   const int lane = threadIdx.x / kScen;
   double sum = 0;
   if (s < n_scen)
@@ -1371,16 +1373,16 @@ __device__ __forceinline__ void store_places(uint16_t *p, I s, I beg, I end, con
 template <int NV, int WR>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, int64_t n_scen, const float *u,
                                                                  int64_t ld_u, uint16_t *place, int64_t ld_place,
-                                                                 Pieces ps, int levels) {
+                                                                 Pieces ps, int levels, uint32_t first) {
   constexpr int E = 8, kRows = kThreads / 64 / WR, kNodes = 64 * NV;  // E: consecutive scenarios of a lane
   __shared__ float lds[kRows * kNodes];
   __shared__ int lds_ok[kRows];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, of_row = wave % WR;
   float *tree = lds + wave / WR * kNodes;
-  const uint32_t vb = blockIdx.x / ps.n;
+  const uint32_t block = first + blockIdx.x, vb = block / ps.n;
   const int64_t v = (int64_t)vb * kRows + wave / WR;
   if (v >= a.n_ops) return;  // with WR > 1 a block has one row
-  const Piece pc = piece_of(a, ps, n_scen, blockIdx.x - vb * ps.n);
+  const Piece pc = piece_of(a, ps, n_scen, block - vb * ps.n);
   if (pc.beg >= pc.end) return;
   const float *pu = u + v * ld_u + pc.beg;
   uint16_t *pp = place + v * ld_place + pc.beg;
@@ -1457,11 +1459,12 @@ __device__ __forceinline__ void row_grad(const RowExp<NV> &row, const float (&x)
 // 48 bf16 take 273 us, 4.8 TB/s in and out (304 without the load ahead).
 template <int G, int NV, bool ONE>
 __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t n_scen, const uint16_t *place,
-                                                          int64_t ld_place, const float *weight, PolicyOut grad, Tile t) {
+                                                          int64_t ld_place, const float *weight, PolicyOut grad, Tile t,
+                                                          uint32_t first) {
   const int g = threadIdx.x % G, grp = threadIdx.x / G;
   const int np = 1 << t.log_pol, nv = (kThreads / G) >> t.log_pol;
-  const uint32_t pol_tiles = ((uint32_t)a.n_pol + np - 1) >> t.log_pol, v_tile = blockIdx.x / pol_tiles;
-  const uint32_t pol = ((blockIdx.x - v_tile * pol_tiles) << t.log_pol) + (grp & (np - 1));
+  const uint32_t block = first + blockIdx.x, pol_tiles = ((uint32_t)a.n_pol + np - 1) >> t.log_pol, v_tile = block / pol_tiles;
+  const uint32_t pol = ((block - v_tile * pol_tiles) << t.log_pol) + (grp & (np - 1));
   const int64_t v0 = (int64_t)v_tile * nv * t.per + (grp >> t.log_pol);
   if (pol >= (uint32_t)a.n_pol) return;
   const float T = policy_temperature(a, (int)pol);
@@ -1553,13 +1556,13 @@ template <int NV, int WR>
 __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
                                                                int64_t ld_place, const float *weight, const float *peak,
                                                                PolicyOut grad, double *part, uint32_t tiles,
-                                                               uint32_t splits, int64_t per_split) {
+                                                               uint32_t splits, int64_t per_split, uint32_t first) {
   using S = GradShape<NV, WR>;
   constexpr int C = S::kColumns, RB = S::kRows, E = 8;
   extern __shared__ double lds_table[];
   const int R = a.n_res, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int t = threadIdx.x % (64 * WR);  // of the group's lanes
-  const uint32_t id = blockIdx.x * S::kGroups + wave / WR;
+  const uint32_t id = (first + blockIdx.x) * S::kGroups + wave / WR;
   const uint32_t tile = id / splits, k = id - tile * splits;
   if (tile >= tiles) return;  // with WR = 4 a block is one group
   const uint32_t per_pol = ((uint32_t)a.n_ops + RB - 1) / RB, pol = tile / per_pol, v0 = (tile - pol * per_pol) * RB;
@@ -1687,9 +1690,9 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
 // The splits' sums of every row joined in order, and its gradient.
 template <int G, int NV>
 __global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, const double *part, uint32_t splits,
-                                                               uint32_t rows, PolicyOut grad) {
+                                                               uint32_t rows, PolicyOut grad, uint32_t first) {
   const int g = threadIdx.x % G, r0 = g * NV;
-  const uint32_t row_id = blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  const uint32_t row_id = (first + blockIdx.x) * (kThreads / G) + threadIdx.x / G;
   if (row_id >= rows) return;
   const uint32_t pol = row_id / (uint32_t)a.n_ops, v = row_id - pol * (uint32_t)a.n_ops;
   const float T = policy_temperature(a, (int)pol);
@@ -1860,6 +1863,19 @@ int launched() { return hipGetLastError() == hipSuccess ? SIM_OK : SIM_E_HIP; }
 
 constexpr int64_t kMaxBlocks = INT32_MAX;
 
+// A launch holds fewer than 2^32 threads, and more are cut off without an error:
+// a grid goes out in launches of up to 2^23 blocks, which are told the first.
+constexpr int64_t kLaunchBlocks = 1 << 23;
+
+template <class F>
+int launch_blocks(int64_t blocks, F f) {
+  for (int64_t first = 0; first < blocks; first += kLaunchBlocks) {
+    f(dim3((unsigned)std::min(blocks - first, kLaunchBlocks)), (uint32_t)first);
+    if (int rc = launched()) return rc;
+  }
+  return SIM_OK;
+}
+
 // Row kernels: up to `side` policies (logp: scenarios) side by side, the other
 // groups along the ops, so that a wavefront's rows lie in few places.  Draws of
 // short rows have 16 side by side, which write 32 bytes of places together, and
@@ -1923,7 +1939,7 @@ bool sample_by_rows(const PolicyArgs &a, int64_t n_scen) {
   const double us = kPerUs;
   const double groups = std::max(rows * lanes / 64 * (300 + 200 * rounds), rounds * 0.8 * us);
   const double waves = std::max((double)a.n_ops * n_scen / std::min<int64_t>(run, 4096) * 450 * std::max<int64_t>(1, lanes / 16), 6 * us);
-  return groups <= waves || (double)a.n_ops * n_scen / run > 1e9;  // blocks of a launch
+  return groups <= waves || (double)a.n_ops * n_scen / run > 1e9;  // blocks of a grid
 }
 
 // Whether a gradient's scenarios are added by groups of lanes in registers (38
@@ -1996,11 +2012,12 @@ int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, in
     if (blocks > kMaxBlocks) return SIM_E_LIMIT;
     const int levels = log2_at_least(a.n_res, SIM_MAX_RES);
     return by_wave(a.n_res, [&](auto NV) {
-      if (wr == 4)
-        k_policy_sample_runs<NV(), 4><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, levels);
-      else
-        k_policy_sample_runs<NV(), 1><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, levels);
-      return launched();
+      return launch_blocks(blocks, [&](dim3 grid, uint32_t first) {
+        if (wr == 4)
+          k_policy_sample_runs<NV(), 4><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, levels, first);
+        else
+          k_policy_sample_runs<NV(), 1><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, ps, levels, first);
+      });
     });
   }
   Tile t;
@@ -2008,12 +2025,12 @@ int launch_policy_sample(const PolicyArgs &a, int64_t n_scen, const float *u, in
   if (int rc = row_tile(a, a.n_res <= 64 ? 16 : 4, t, blocks)) return rc;
   return by_row(a.n_res, [&](auto G, auto NV) {
     auto go = [&](auto cuts) {
-      const dim3 grid((unsigned)blocks), block(kThreads);
-      if (one)
-        k_policy_sample_one<G(), NV(), cuts()><<<grid, block, 0, st>>>(a, n_scen, u, ld_u, place, ld_place, t);
-      else
-        k_policy_sample_few<G(), NV(), cuts()><<<grid, block, 0, st>>>(a, n_scen, u, ld_u, place, ld_place, t);
-      return launched();
+      return launch_blocks(blocks, [&](dim3 grid, uint32_t first) {
+        if (one)
+          k_policy_sample_one<G(), NV(), cuts()><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, t, first);
+        else
+          k_policy_sample_few<G(), NV(), cuts()><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, u, ld_u, place, ld_place, t, first);
+      });
     };
     return cut ? go(std::true_type{}) : go(std::false_type{});
   });
@@ -2038,35 +2055,36 @@ int64_t policy_work(const PolicyArgs &a, int64_t n_scen) {
 
 int launch_policy_logp(const PolicyArgs &a, int64_t n_scen, const uint16_t *place, int64_t ld_place, float *logp,
                        void *work, hipStream_t st) {
-  const int64_t join = (n_scen + kJoinScen - 1) / kJoinScen;
-  if (join > kMaxBlocks) return SIM_E_LIMIT;
+  auto join = [&](auto *part, int64_t chunks) {
+    return launch_blocks((n_scen + kJoinScen - 1) / kJoinScen, [&](dim3 grid, uint32_t first) {
+      k_policy_join<<<grid, dim3(kThreads), 0, st>>>(part, chunks, n_scen, logp, first);
+    });
+  };
   if (long_runs(a, n_scen)) {
     const LogpRuns l = logp_runs(a, n_scen);
-    if (l.pieces * l.chunks > kMaxBlocks) return SIM_E_LIMIT;
+    const int64_t blocks = l.pieces * l.chunks;
+    if (blocks > kMaxBlocks) return SIM_E_LIMIT;
     float *to = l.chunks > 1 ? (float *)work : logp;
-    const dim3 grid((unsigned)(l.pieces * l.chunks));
     const int rc = by_row(a.n_res, [&](auto G, auto NV) {
-      if (l.wide)
-        k_policy_logp_runs<G(), NV(), 8><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.ops_per);
-      else
-        k_policy_logp_runs<G(), NV(), 1><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.ops_per);
-      return launched();
+      return launch_blocks(blocks, [&](dim3 grid, uint32_t first) {
+        if (l.wide)
+          k_policy_logp_runs<G(), NV(), 8><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.ops_per, first);
+        else
+          k_policy_logp_runs<G(), NV(), 1><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, to, l.ps, l.ops_per, first);
+      });
     });
-    if (rc || l.chunks == 1) return rc;
-    k_policy_join<<<dim3((unsigned)join), dim3(kThreads), 0, st>>>((const float *)work, l.chunks, n_scen, logp);
-    return launched();
+    return rc || l.chunks == 1 ? rc : join((const float *)work, l.chunks);
   }
   Tile t;
   int64_t blocks;
   const int64_t chunks = logp_tile(a, n_scen, t, blocks);
   if (blocks > kMaxBlocks) return SIM_E_LIMIT;
-  int rc = by_row(a.n_res, [&](auto G, auto NV) {
-    k_policy_logp<G(), NV()><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, (double *)work, t);
-    return launched();
+  const int rc = by_row(a.n_res, [&](auto G, auto NV) {
+    return launch_blocks(blocks, [&](dim3 grid, uint32_t first) {
+      k_policy_logp<G(), NV()><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, (double *)work, t, first);
+    });
   });
-  if (rc) return rc;
-  k_policy_join<<<dim3((unsigned)join), dim3(kThreads), 0, st>>>((const double *)work, chunks, n_scen, logp);
-  return launched();
+  return rc ? rc : join((const double *)work, chunks);
 }
 
 int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *place, int64_t ld_place,
@@ -2082,30 +2100,33 @@ int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
     auto go = [&](auto NV, auto WR) {
       using S = GradShape<NV(), WR()>;
       const uint32_t tiles = (uint32_t)(a.n_pol * ((a.n_ops + (int64_t)S::kRows - 1) / S::kRows));
-      const uint32_t blocks = (uint32_t)(((int64_t)tiles * splits + S::kGroups - 1) / S::kGroups);
-      k_policy_grad_runs<NV(), WR()><<<dim3(blocks), dim3(kThreads), S::lds(a.n_res), st>>>(
-          a, n_scen, place, ld_place, weight, peak, grad, part, tiles, splits, r.per_split);
-      return launched();
+      const int64_t blocks = ((int64_t)tiles * splits + S::kGroups - 1) / S::kGroups;
+      return launch_blocks(blocks, [&](dim3 grid, uint32_t first) {
+        k_policy_grad_runs<NV(), WR()><<<grid, dim3(kThreads), S::lds(a.n_res), st>>>(
+            a, n_scen, place, ld_place, weight, peak, grad, part, tiles, splits, r.per_split, first);
+      });
     };
     int rc = by_wave(a.n_res, [&](auto NV) {
       return r.waves == 4 ? go(NV, std::integral_constant<int, 4>{}) : go(NV, std::integral_constant<int, 1>{});
     });
     if (rc || splits == 1) return rc;
     return by_row(a.n_res, [&](auto G, auto NV) {
-      const unsigned per = kThreads / G();
-      k_policy_grad_join<G(), NV()><<<dim3((rows + per - 1) / per), dim3(kThreads), 0, st>>>(a, part, splits, rows, grad);
-      return launched();
+      const int64_t per = kThreads / G();
+      return launch_blocks((r.rows + per - 1) / per, [&](dim3 grid, uint32_t first) {
+        k_policy_grad_join<G(), NV()><<<grid, dim3(kThreads), 0, st>>>(a, part, splits, rows, grad, first);
+      });
     });
   }
   Tile t;
   int64_t blocks;
   if (int rc = row_tile(a, 4, t, blocks)) return rc;
   return by_row(a.n_res, [&](auto G, auto NV) {
-    if (a.block == 1 && n_scen <= a.period)
-      k_policy_grad<G(), NV(), true><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t);
-    else
-      k_policy_grad<G(), NV(), false><<<dim3((unsigned)blocks), dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t);
-    return launched();
+    return launch_blocks(blocks, [&](dim3 grid, uint32_t first) {
+      if (a.block == 1 && n_scen <= a.period)
+        k_policy_grad<G(), NV(), true><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t, first);
+      else
+        k_policy_grad<G(), NV(), false><<<grid, dim3(kThreads), 0, st>>>(a, n_scen, place, ld_place, weight, grad, t, first);
+    });
   });
 }
 

@@ -4,6 +4,7 @@ time, with the error bounds that the GPU tests hold the kernels to.
 EPS is half a step of float32: every float32 operation is off by at most EPS
 relative to its result, the exponential and the logarithm by a few of them."""
 import numpy as np
+import torch
 
 EPS = 2.0**-24
 #: half a step of the type that a gradient is rounded to
@@ -188,3 +189,54 @@ def near(got, want, tol, what):
     fine = np.isfinite(want)
     off = np.abs(got[fine] - want[fine]) - np.broadcast_to(tol, want.shape)[fine]
     assert not (off > 0).any() and np.isfinite(got[fine]).all(), f"{what}: {off.max():.3g} over the bound"
+
+
+# One scenario a policy, all rows at once (torch, 64 bits, on the logits' device).
+
+
+def sample_each(x, u, settings):
+    """int64 [n_ops, n_pol] from float64 x [n_pol, n_ops, n_res], u [n_ops, n_pol]."""
+    T, k, p, m = (settings[:, i, None, None] for i in range(4))
+    bad = (x.isnan() | (x == float("inf"))).any(-1) | (x == -float("inf")).all(-1)
+    bad |= ~((T >= 0) & (T < float("inf")) & (k >= 0) & (p >= 0) & (p <= 1) & (m >= 0) & (m <= 1))[..., 0]
+    one = (T == 0) | (p == 0)
+    k = k.floor().masked_fill(k < 1, x.shape[-1]).masked_fill(one, 1)
+    p = p.masked_fill(one, 1)
+    T = T.masked_fill(T == 0, 1)
+    x = x + 0.0  # -0 and 0 are the same logit
+    s, order = x.sort(dim=-1, descending=True, stable=True)
+    w = ((s - s[..., :1]) / T).exp()
+    at = torch.arange(x.shape[-1], device=x.device)
+    keep = (s > -float("inf")) & (at < k)
+    c = (w * keep).cumsum(-1)
+    before = torch.cat([torch.zeros_like(c[..., :1]), c[..., :-1]], -1)
+    keep &= (before < p * c[..., -1:]) | (p >= 1) | (at == 0)
+    keep &= (w >= m) | (at == 0)
+    kept = torch.zeros_like(w).scatter_(-1, order, w * keep)
+    c = kept.cumsum(-1)
+    u = u.T[..., None]
+    place = (c <= u.clamp(min=0) * c[..., -1:]).sum(-1)
+    place = torch.minimum(place, torch.where(kept > 0, at, 0).amax(-1))
+    return place.masked_fill(bad | u[..., 0].isnan(), NO_PLACE).T
+
+
+def learn_each(x, place, weight, T, dtype):
+    """(logp [n_pol], bound, grad, bound) from float64 x, int64 place [n_ops,
+    n_pol], float64 weight [n_pol] and T [n_pol]; bounds as logp's and grad's."""
+    z = (x - x.amax(-1, keepdim=True)) / T[:, None, None]
+    allowed = x > -float("inf")
+    lse = z.exp().sum(-1, keepdim=True).log()
+    lp = z - lse
+    at = place.T[..., None]
+    there = at < x.shape[-1]
+    at = at.clamp(max=x.shape[-1] - 1)
+    t = torch.where(there, lp.gather(-1, at), -float("inf"))[..., 0]
+    za = torch.where(allowed, z.abs(), 0)
+    off = EPS * (33 * t.abs() + 4 * za.gather(-1, at)[..., 0] + 40)
+    w = weight[:, None, None]
+    h = torch.zeros_like(x).scatter_(-1, at, w * there) * allowed
+    W, pi, T = h.sum(-1, keepdim=True), lp.exp(), T[:, None, None]
+    g = torch.where(allowed, (h - W * pi) / T, 0)
+    d = EPS * (h.abs() + 31 * pi * W.abs() + W.abs() * pi * (4 * za + 44) + 2 * (h.abs() + W.abs() * pi)) + W.abs() * TINY
+    d = d / T + 4 * EPS * g.abs()
+    return t.sum(-1), off.sum(-1), g, d + HALF_STEP[dtype] * (g.abs() + d) + HALF_TINY[dtype]

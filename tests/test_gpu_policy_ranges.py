@@ -1,0 +1,73 @@
+"""GPU placement policies over the ranges that a call may have: the largest
+grids, weights and logits of very different size, rows of every length with a
+scenario of their own.  Against the plain 64-bit forms of policy_ref.py."""
+import numpy as np
+import pytest
+
+import policy_ref as ref
+from test_gpu_policy import host16, make_logits, mlsim  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+# A launch holds fewer than 2^32 threads, 2^24 blocks of 256.  Each of the four
+# below has more blocks.
+
+
+def test_draws_of_more_blocks_than_a_launch_holds(mlsim):
+    """Two policies in turn over 2000001 scenarios: 22 million blocks."""
+    P, N, R, S = 2, 42, 3, 2_000_001
+    rng = np.random.default_rng(31)
+    t, x = make_logits(rng, P, N, R, "float32")
+    u = torch.rand((N, S), device="cuda", generator=torch.Generator("cuda").manual_seed(31))
+    got = host16(mlsim.Policy(t).sample(u))
+    st = ref.settings_of(P)
+    for v in range(0, N, 5):
+        want = ref.sample(x[:, v:v + 1], u[v:v + 1].cpu().numpy().astype(np.float64), st)
+        assert np.array_equal(got[v:v + 1], want), v
+
+
+def test_logp_of_more_blocks_than_a_launch_holds(mlsim):
+    """2^28 + 1000 scenarios of two policies in turn: four a block, and sixteen
+    a block where the ops' parts are joined."""
+    P, R, S = 2, 9, 2**28 + 1000
+    rng = np.random.default_rng(32)
+    t, x = make_logits(rng, P, 1, R, "float32", masked=False)
+    place = torch.randint(0, R, (1, S), device="cuda", dtype=torch.int16, generator=torch.Generator("cuda").manual_seed(32))
+    got = mlsim.Policy(t).logp(place.view(torch.uint16))
+    one = [ref.logp(x[p:p + 1], np.arange(R)[None], ref.settings_of(1)) for p in range(P)]
+    for p in range(P):
+        want, tol = (torch.from_numpy(q).cuda() for q in one[p])
+        for s in range(p, S, 2**26):
+            a = place[0, s:min(S, s + 2**26):2].int()
+            assert ((got[s:min(S, s + 2**26):2].double() - want[a]).abs() <= tol[a]).all(), (p, s)
+
+
+@pytest.mark.parametrize("more", [0, 4])
+def test_rows_of_more_blocks_than_a_launch_holds(mlsim, more):
+    """2^26 + 5 policies that share a row, four to a block: one scenario each,
+    then a second for some."""
+    P, R = 2**26 + 5, 520
+    S = P + more
+    rng = np.random.default_rng(33)
+    t, x = make_logits(rng, 1, 1, R, "bfloat16")
+    u = torch.rand((1, S), device="cuda", generator=torch.Generator("cuda").manual_seed(33))
+    got = mlsim.Policy(t.expand(P, 1, R)).sample(u)
+    C, last = ref.kept_sums(x[0, 0], 1.0, 0, 1.0, 0.0)
+    C = torch.from_numpy(C).cuda()
+    want = torch.searchsorted(C, u[0].double() * C[-1], right=True).clamp(max=last)
+    assert torch.equal(got[0].view(torch.int16).int(), want.int())
+
+
+def test_gradients_of_more_blocks_than_a_launch_holds(mlsim):
+    P, R = 2**26 + 5, 2
+    gen = torch.Generator("cuda").manual_seed(34)
+    x = torch.randn((P, 1, R), device="cuda", generator=gen).bfloat16()
+    w = torch.randn(P, device="cuda", generator=gen)
+    a = torch.randint(0, R, (1, P), device="cuda", dtype=torch.int16, generator=gen)
+    got = mlsim.Policy(x).grad(a.view(torch.uint16), w)
+    for s in range(0, P, 2**24):
+        e = min(P, s + 2**24)
+        _, _, g, tol = ref.learn_each(x[s:e].double(), a[:, s:e].long(), w[s:e].double(), torch.ones(e - s, device="cuda").double(), "bfloat16")
+        assert ((got[s:e].double() - g).abs() <= tol).all(), s

@@ -158,3 +158,34 @@ def test_temperatures_and_numbers_of_scenarios(L):
         assert L.sim_policy_work(struct(temperature=T), 8) == mlsim.SIM_E_INVAL
     assert L.sim_policy_work(struct(), 2**30) >= 0
     assert L.sim_policy_work(struct(), 2**30 + 1) == mlsim.SIM_E_LIMIT
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_plain_forms_of_one_scenario_a_policy(dtype):
+    """The forms over all rows at once against those row by row."""
+    rng = np.random.default_rng(5)
+    P, N, R = 9, 8, 11
+    x = rng.normal(size=(P, N, R)) * 2
+    x[rng.random((P, N, R)) < 0.2] = -np.inf
+    x[:, ::3] = np.round(x[:, ::3])
+    x[:, 1] = np.where(rng.random((P, R)) < 0.5, 0.0, -0.0)
+    x[0, 2], x[1, 2, 3], x[2, 2, 4] = -np.inf, np.nan, np.inf
+    u = (rng.integers(0, 2**24, (N, P)) * 2.0**-24)
+    u[3, :4] = [-1.0, np.nan, 1.0, 0.0]
+    for cut in (dict(), dict(top_k=3), dict(temperature=0.7, top_k=4, top_p=0.8), dict(min_p=0.2), dict(temperature=0.0), dict(top_p=0.0),
+                dict(temperature=rng.choice([0.0, 0.5, -1.0, 3.0], P), top_k=rng.integers(-1, R + 2, P), top_p=rng.random(P) * 1.1, min_p=rng.random(P))):
+        st = ref.settings_of(P, **cut)
+        got = ref.sample_each(torch.from_numpy(x), torch.from_numpy(u), torch.from_numpy(st))
+        assert np.array_equal(got.numpy(), ref.sample(x, u, st)), cut
+    x[0, 2], x[1, 2, 3], x[2, 2, 4] = 1.0, 0.0, 0.0
+    a = rng.integers(0, R + 1, (N, P))
+    a[:, :4] = np.argmax(x, -1).T[:, :4]
+    w, T = rng.normal(size=P), rng.choice([0.5, 1.0, 3.0], P)
+    lp, ltol, g, gtol = (q.numpy() for q in ref.learn_each(torch.from_numpy(x), torch.from_numpy(a), torch.from_numpy(w), torch.from_numpy(T), dtype))
+    want, tol = ref.logp(x, a, ref.settings_of(P, T))
+    ref.near(lp, want, 1e-12, "logp")
+    fine = np.isfinite(want)
+    assert np.allclose(ltol[fine], tol[fine], rtol=1e-12, atol=0)
+    want, tol = ref.grad(x, a, w, ref.settings_of(P, T), dtype=dtype)
+    ref.near(g, want, 1e-12, "grad")
+    assert (gtol < 4 * tol + 1e-30).all() and (tol < 4 * gtol + 1e-30).all()
