@@ -493,8 +493,8 @@ int sim_policy_logp(const sim_policy *p, int64_t n_scen, const uint16_t *place, 
  * W the sum of the row's h_r; 0 where the logit is -inf.  A place >= n_res or
  * on a logit of -inf adds nothing.  Invalid rows and T = 0 give NaN.
  *   weight  device float32 [n_scen].  Where many scenarios share a row, weights
- *           are first rounded to multiples of at most 2^-29 of the largest one
- *           (2^-37 at 16384 scenarios), so that their sums are exact.
+ *           are first rounded to multiples of at most 2^-29 of their policy's
+ *           largest one (2^-37 at 16384 scenarios), so that their sums are exact.
  *   grad    device [n_pol][n_ops][n_res] of `dtype`, written whole: strides
  *           ld_gpol and ld_gop in elements, no row over another.
  *   work    as sim_policy_logp.

@@ -1511,20 +1511,27 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
   });
 }
 
-// The largest magnitude of the weights of each block's share (NaN counts as
-// infinite), for the grid below.
-constexpr int kPeakBlocks = 64;
-__global__ __launch_bounds__(kThreads) void k_policy_peak(const float *weight, int64_t n, float *peak) {
+// The largest magnitude of each policy's weights (NaN counts as infinite), for
+// the grid below: peak[p][part], of the scenarios whose number in their policy
+// lies in every `parts`th block of threads.
+__global__ __launch_bounds__(kThreads) void k_policy_peak(PolicyArgs a, int64_t n_scen, const float *weight, uint32_t parts, float *peak,
+                                                          uint32_t first) {
   __shared__ float red[kThreads / 64];
+  const uint32_t block = first + blockIdx.x, pol = block / parts, threads = blockDim.x;
+  const PolicyScenarios scenario(a, (int)pol, n_scen);
   float m = 0;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
-    const float w = fabsf(weight[i]);
+  for (uint32_t i = (block - pol * parts) * threads + threadIdx.x; i < n_scen; i += parts * threads) {
+    const int64_t s = scenario((int)i);
+    if (s < 0) break;
+    const float w = fabsf(weight[s]);
     m = w == w ? fmaxf(m, w) : kInf;
   }
   m = group_max<64>(m);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
   __syncthreads();
-  if (threadIdx.x == 0) peak[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  if (threadIdx.x) return;
+  for (uint32_t i = 1; i < threads / 64; ++i) m = fmaxf(m, red[i]);
+  peak[block] = m;
 }
 
 // A block of the kernel below has four wavefronts.  Together (WR = 4) they take
@@ -1543,8 +1550,9 @@ struct GradShape {
 // resource in a table of LDS of float64 for every row.  A weight is first
 // rounded to a grid on which every sum of a split is exact, so that the lanes'
 // order does not matter and any of them may add to any entry: with the largest
-// weight below 2^E and fewer than 2^L scenarios, multiples of 2^(E + L - 53) (an
-// error of at most 2^-38 of the largest at 16384 scenarios, 2^-30 at most).
+// weight of the row's policy below 2^E and fewer than 2^L scenarios, multiples of
+// 2^(E + L - 53) (an error of at most 2^-38 of the largest at 16384 scenarios,
+// 2^-30 at most).
 // Columns keep down how many lanes meet in one entry.  (An LDS addition of
 // float64 takes 9 clocks for a wavefront with 16 columns or more, 17 with 8, 20
 // with 4; one of float32 takes 193, 3 a lane.)  Then a wavefront adds up a row's
@@ -1555,7 +1563,7 @@ struct GradShape {
 template <int NV, int WR>
 __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
                                                                int64_t ld_place, const float *weight, const float *peak,
-                                                               PolicyOut grad, double *part, uint32_t tiles,
+                                                               uint32_t parts, PolicyOut grad, double *part, uint32_t tiles,
                                                                uint32_t splits, int64_t per_split, uint32_t first) {
   using S = GradShape<NV, WR>;
   constexpr int C = S::kColumns, RB = S::kRows, E = 8;
@@ -1576,7 +1584,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
   if (finish && splits == 1)
     load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, lane * NV, R, x);
   for (int i = t; i < RB * R * C; i += 64 * WR) table[i] = 0;
-  const float top = group_max<64>(peak[lane]);
+  const float top = group_max<64>(peak[(uint64_t)pol * parts + min((uint32_t)lane, parts - 1)]);
   // adding and taking away 1.5 2^52 grid steps rounds to the grid
   const double magic = top > 0 && top < kInf ? ldexp(1.5, ilogbf(top) + 64 - __clzll(per_split)) : 0.0;
   if (WR > 1)
@@ -1980,6 +1988,8 @@ LogpRuns logp_runs(const PolicyArgs &a, int64_t n_scen) {
 struct GradRuns {
   int64_t rows, splits, per_split;
   int waves;  // of a row
+  uint32_t parts;         // of a policy's weights, for their peak
+  int64_t peak_bytes;
 };
 
 // Enough wavefronts to fill the chip, none with fewer than 2048 scenarios of
@@ -1993,6 +2003,8 @@ GradRuns grad_runs(const PolicyArgs &a, int64_t n_scen) {
   r.splits = std::max(r.splits, (n_scen + (1 << 22) - 1) >> 22);
   r.per_split = ((n_scen + r.splits - 1) / r.splits + 511) / 512 * 512;
   r.splits = (n_scen + r.per_split - 1) / r.per_split;
+  r.parts = (uint32_t)std::min<int64_t>(64, std::max(1, 4096 / a.n_pol));
+  r.peak_bytes = ((int64_t)a.n_pol * r.parts * 4 + 7) / 8 * 8;
   return r;
 }
 
@@ -2048,7 +2060,7 @@ int64_t policy_work(const PolicyArgs &a, int64_t n_scen) {
   }
   if (!grad_by_rows(a, n_scen)) {
     const GradRuns r = grad_runs(a, n_scen);
-    grad = kPeakBlocks * 4 + (r.splits > 1 ? r.splits * r.rows * a.n_res * 8 : 0);
+    grad = r.peak_bytes + (r.splits > 1 ? r.splits * r.rows * a.n_res * 8 : 0);
   }
   return (std::max(logp, grad) + 7) / 8 * 8;
 }
@@ -2091,19 +2103,23 @@ int launch_policy_grad(const PolicyArgs &a, int64_t n_scen, const uint16_t *plac
                        const float *weight, const PolicyOut &grad, void *work, hipStream_t st) {
   if (!grad_by_rows(a, n_scen)) {
     const GradRuns r = grad_runs(a, n_scen);
-    if (r.rows * r.splits > kMaxBlocks) return SIM_E_LIMIT;
+    const int64_t peak_blocks = a.n_pol * (int64_t)r.parts;
+    if (std::max(r.rows * r.splits, peak_blocks) > kMaxBlocks) return SIM_E_LIMIT;
     float *peak = (float *)work;
-    double *part = (double *)((char *)work + kPeakBlocks * 4);
+    double *part = (double *)((char *)work + r.peak_bytes);
     const uint32_t rows = (uint32_t)r.rows, splits = (uint32_t)r.splits;
-    k_policy_peak<<<dim3(kPeakBlocks), dim3(kThreads), 0, st>>>(weight, n_scen, peak);
-    if (int rc = launched()) return rc;
+    const dim3 threads(r.waves * 64);  // under 2048 scenarios a policy need no more than a wavefront
+    if (int rc = launch_blocks(peak_blocks, [&](dim3 grid, uint32_t first) {
+          k_policy_peak<<<grid, threads, 0, st>>>(a, n_scen, weight, r.parts, peak, first);
+        }))
+      return rc;
     auto go = [&](auto NV, auto WR) {
       using S = GradShape<NV(), WR()>;
       const uint32_t tiles = (uint32_t)(a.n_pol * ((a.n_ops + (int64_t)S::kRows - 1) / S::kRows));
       const int64_t blocks = ((int64_t)tiles * splits + S::kGroups - 1) / S::kGroups;
       return launch_blocks(blocks, [&](dim3 grid, uint32_t first) {
         k_policy_grad_runs<NV(), WR()><<<grid, dim3(kThreads), S::lds(a.n_res), st>>>(
-            a, n_scen, place, ld_place, weight, peak, grad, part, tiles, splits, r.per_split, first);
+            a, n_scen, place, ld_place, weight, peak, r.parts, grad, part, tiles, splits, r.per_split, first);
       });
     };
     int rc = by_wave(a.n_res, [&](auto NV) {

@@ -191,6 +191,45 @@ def near(got, want, tol, what):
     assert not (off > 0).any() and np.isfinite(got[fine]).all(), f"{what}: {off.max():.3g} over the bound"
 
 
+def grid_of(weight, n_scen):
+    """The largest step that a weight may be rounded to where scenarios share a
+    row: sums of up to min(n_scen rounded up to 512, 2^22) weights below 2^(e + 1) are exact
+    in float64 on multiples of 2^(e + L - 52), for L the bits of that count; e is
+    of the largest finite weight of the policy."""
+    w = np.abs(weight[np.isfinite(weight)])
+    if not w.size or not w.max():
+        return 0.0
+    n = min(-(-n_scen // 512) * 512, 2**22)
+    return 2.0 ** (np.floor(np.log2(w.max())) + n.bit_length() - 52)
+
+
+def grad_shared(logits, place, weight, settings, block=1, scen0=0, dtype="float32"):
+    """(grad, bound) where weights are rounded to the grid and their sums exact:
+    a resource's sum of n weights is off by n half steps and one rounding to
+    float32, W by 30 roundings more, pi as in logp."""
+    P, N, R = logits.shape
+    S = place.shape[1]
+    pol = policy_of(np.arange(S), block, scen0, P)
+    g, tol = np.zeros((P, N, R)), np.zeros((P, N, R))
+    for p in range(P):
+        at = np.flatnonzero(pol == p)
+        T, w = settings[p, 0], weight[at].astype(np.float64)
+        half = grid_of(w, S) / 2
+        for v in range(N):
+            lp, z = log_pi(logits[p, v], T)
+            allowed = logits[p, v] > -np.inf
+            a = place[v, at]
+            ok = a < R
+            h = np.bincount(a[ok], w[ok], R)[:R] * allowed
+            d_h = (np.bincount(a[ok], minlength=R)[:R] * half + EPS * np.abs(h)) * allowed
+            W, pi = h.sum(), np.exp(lp)
+            g[p, v] = np.where(allowed, (h - W * pi) / T, 0)
+            d = d_h + pi * (d_h.sum() + 30 * EPS * np.abs(h).sum()) + np.abs(W) * pi * EPS * (4 * np.abs(z) + 44)
+            d = (d + EPS * 2 * (np.abs(h) + np.abs(W) * pi) + np.abs(W) * TINY) / T + 4 * EPS * np.abs(g[p, v])
+            tol[p, v] = (d + HALF_STEP[dtype] * (np.abs(g[p, v]) + d) + HALF_TINY[dtype]) * allowed
+    return g, tol
+
+
 # One scenario a policy, all rows at once (torch, 64 bits, on the logits' device).
 
 

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 import policy_ref as ref
-from test_gpu_policy import host16, make_logits, mlsim  # noqa: F401
+from test_gpu_policy import draws, host16, make_logits, mlsim, u16  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -71,3 +71,62 @@ def test_gradients_of_more_blocks_than_a_launch_holds(mlsim):
         e = min(P, s + 2**24)
         _, _, g, tol = ref.learn_each(x[s:e].double(), a[:, s:e].long(), w[s:e].double(), torch.ones(e - s, device="cuda").double(), "bfloat16")
         assert ((got[s:e].double() - g).abs() <= tol).all(), s
+
+
+# (policies, ops, resources, scenarios per run, scenarios): long runs, short runs,
+# a wavefront a row, and batches split over the scenarios
+SHARED = [(2, 5, 40, 16384, 32768), (3, 40, 64, 5000, 15000), (2, 3, 9, 3, 60001), (2, 300, 64, 200, 400), (4, 5, 64, 700, 20011),
+          (3, 2, 600, 1, 30001), (2, 2000, 100, 5000, 10000)]
+
+
+@pytest.mark.parametrize("shape", SHARED, ids=str)
+def test_gradients_of_weights_of_different_size(mlsim, shape):
+    """Each policy's weights are 10^10 times the next one's: a gradient is as
+    exact as if its policy were alone."""
+    P, N, R, block, S = shape
+    rng = np.random.default_rng(41)
+    t, x = make_logits(rng, P, N, R, "float32")
+    a = draws(rng, x, S)
+    pol = ref.policy_of(np.arange(S), block, 0, P)
+    w = (rng.normal(size=S) * 10.0 ** (8 - 10 * pol)).astype(np.float32)
+    got = mlsim.Policy(t, block=block).grad(u16(a), torch.from_numpy(w).cuda())
+    g, tol = ref.grad_shared(x, a, w, ref.settings_of(P), block)
+    ref.near(got.double().cpu().numpy(), g, tol, f"grad {shape}")
+    assert ((np.abs(g) > 4 * tol) | (x == -np.inf)).mean() > 0.9  # zeros would not pass
+
+
+def cancelling(rng, a, w, at):
+    """Weights of the scenarios `at` whose large ones cancel place by place: what
+    the small ones add depends on the order of the additions, unless all are
+    first rounded to a grid (to which the small ones are 0)."""
+    n = len(at) // 3 * 3
+    x, y, z = at[0:n:3], at[1:n:3], at[2:n:3]
+    a[:, y] = a[:, x]
+    w[x] = rng.choice([-1, 1], len(x)) * 2.0**60
+    w[y], w[z] = -w[x], rng.choice([-1, 1], len(z))
+    w[at[n:]] = 0
+
+
+@pytest.mark.parametrize("shape", SHARED, ids=str)
+def test_gradients_beside_weights_that_are_not_finite(mlsim, shape):
+    """An infinite weight and a NaN of one policy: its own gradients show them,
+    those of the others have the same bits as without, every time."""
+    P, N, R, block, S = shape
+    rng = np.random.default_rng(42)
+    t, x = make_logits(rng, P, N, R, "float32")
+    a = draws(rng, x, S)
+    pol = ref.policy_of(np.arange(S), block, 0, P)
+    w = rng.normal(size=S).astype(np.float32)
+    for p in [p for p in range(P) if p != 1]:
+        cancelling(rng, a, w, np.flatnonzero(pol == p))
+    place = u16(a)
+    policy = mlsim.Policy(t, block=block)
+    want = policy.grad(place, torch.from_numpy(w).cuda())
+    ref.near(want.double().cpu().numpy(), *ref.grad_shared(x, a, w, ref.settings_of(P), block), f"grad {shape}")
+    mine = np.flatnonzero(pol == 1)
+    w[mine[5]], w[mine[70]] = np.inf, np.nan
+    others = [p for p in range(P) if p != 1]
+    for _ in range(3):
+        got = policy.grad(place, torch.from_numpy(w).cuda())
+        assert torch.equal(got[others], want[others])
+        assert (~torch.isfinite(got[1]) | torch.isinf(t[1])).all()

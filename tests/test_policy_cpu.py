@@ -189,3 +189,20 @@ def test_plain_forms_of_one_scenario_a_policy(dtype):
     want, tol = ref.grad(x, a, w, ref.settings_of(P, T), dtype=dtype)
     ref.near(g, want, 1e-12, "grad")
     assert (gtol < 4 * tol + 1e-30).all() and (tol < 4 * gtol + 1e-30).all()
+
+
+def test_plain_gradients_of_shared_rows():
+    """The same values as row by row, and a bound that zeros do not pass."""
+    rng = np.random.default_rng(6)
+    x, a, w = rng.normal(size=(2, 3, 7)), rng.integers(0, 8, (3, 4001)), rng.normal(size=4001).astype(np.float32)
+    x[0, 1, 2] = -np.inf
+    st = ref.settings_of(2, [0.5, 2.0])
+    for dtype in ("float32", "float16"):
+        g, tol = ref.grad_shared(x, a, w, st, 5, 3, dtype)
+        ref.near(g, ref.grad(x, a, w.astype(np.float64), st, 5, 3, dtype)[0], 1e-9, "grad")
+        assert ((np.abs(g) > 20 * tol) | (x == -np.inf)).mean() > 0.9
+    assert ref.grid_of(w, 4001) < 2.0**-36 and ref.grid_of(np.zeros(3, np.float32), 3) == 0
+    # the grid: as many of the largest weight as a batch may have add up exactly in float64
+    for n in (1, 512, 4001, 2**22, 2**30):
+        step, count = ref.grid_of(np.array([1.9], np.float32), n), min(-(-n // 512) * 512, 2**22)
+        assert 2.0 * count / step <= 2.0**53
