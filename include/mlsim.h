@@ -494,7 +494,8 @@ int sim_policy_logp(const sim_policy *p, int64_t n_scen, const uint16_t *place, 
  * on a logit of -inf adds nothing.  Invalid rows and T = 0 give NaN.
  *   weight  device float32 [n_scen].  Where many scenarios share a row, weights
  *           are first rounded to multiples of at most 2^-29 of their policy's
- *           largest one (2^-37 at 16384 scenarios), so that their sums are exact.
+ *           largest finite one (2^-37 at 16384 scenarios), so that their sums
+ *           are exact.  Infinite ones and NaN show in their rows only.
  *   grad    device [n_pol][n_ops][n_res] of `dtype`, written whole: strides
  *           ld_gpol and ld_gop in elements, no row over another.
  *   work    as sim_policy_logp.

@@ -1511,9 +1511,9 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad(PolicyArgs a, int64_t 
   });
 }
 
-// The largest magnitude of each policy's weights (NaN counts as infinite), for
-// the grid below: peak[p][part], of the scenarios whose number in their policy
-// lies in every `parts`th block of threads.
+// The largest magnitude of each policy's finite weights, for the grid below:
+// peak[p][part], of the scenarios whose number in their policy lies in every
+// `parts`th block of threads.
 __global__ __launch_bounds__(kThreads) void k_policy_peak(PolicyArgs a, int64_t n_scen, const float *weight, uint32_t parts, float *peak,
                                                           uint32_t first) {
   __shared__ float red[kThreads / 64];
@@ -1524,7 +1524,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_peak(PolicyArgs a, int64_t 
     const int64_t s = scenario((int)i);
     if (s < 0) break;
     const float w = fabsf(weight[s]);
-    m = w == w ? fmaxf(m, w) : kInf;
+    m = w < kInf ? fmaxf(m, w) : m;
   }
   m = group_max<64>(m);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
@@ -1585,8 +1585,9 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
     load_row<NV>(a.logits, a.dtype, pol * a.ld_pol + v * a.ld_op, lane * NV, R, x);
   for (int i = t; i < RB * R * C; i += 64 * WR) table[i] = 0;
   const float top = group_max<64>(peak[(uint64_t)pol * parts + min((uint32_t)lane, parts - 1)]);
-  // adding and taking away 1.5 2^52 grid steps rounds to the grid
-  const double magic = top > 0 && top < kInf ? ldexp(1.5, ilogbf(top) + 64 - __clzll(per_split)) : 0.0;
+  // adding and taking away 1.5 2^52 grid steps rounds to the grid; weights that
+  // are not finite stay, and so do sums with them, in any order
+  const double magic = top > 0 ? ldexp(1.5, ilogbf(top) + 64 - __clzll(per_split)) : 0.0;
   if (WR > 1)
     __syncthreads();
   else
@@ -1678,6 +1679,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int
 #pragma unroll
       for (int c = 0; c < C; ++c) sum[j] += table[(own * R + r0 + j) * C + (lane + c) % C];  // lanes in different banks
     }
+    if (sum[j] != sum[j]) sum[j] = __builtin_nan("");  // of several the first stays: one for all
     h[j] = (float)sum[j];
   }
   if (splits > 1) {

@@ -130,3 +130,34 @@ def test_gradients_beside_weights_that_are_not_finite(mlsim, shape):
         got = policy.grad(place, torch.from_numpy(w).cuda())
         assert torch.equal(got[others], want[others])
         assert (~torch.isfinite(got[1]) | torch.isinf(t[1])).all()
+
+
+@pytest.mark.parametrize("shape", SHARED, ids=str)
+def test_gradients_where_weights_that_are_not_finite_have_no_place(mlsim, shape):
+    """Infinite and NaN weights of scenarios whose ops mostly have no place: the
+    rows where they add nothing have the same bits as without them, the others
+    show them with the same bits every time."""
+    P, N, R, block, S = shape
+    rng = np.random.default_rng(43)
+    t, x = make_logits(rng, P, N, R, "float32")
+    a = draws(rng, x, S)
+    pol = ref.policy_of(np.arange(S), block, 0, P)
+    w = np.zeros(S, np.float32)
+    for p in range(P):
+        at = np.flatnonzero(pol == p)
+        cancelling(rng, a, w, at)
+        w[at[30:33]] = 0
+        a[1:, at[30:33]] = ref.NO_PLACE
+    policy = mlsim.Policy(t, block=block)
+    want = policy.grad(u16(a), torch.from_numpy(w).cuda())
+    for p in range(P):
+        at = np.flatnonzero(pol == p)
+        w[at[30:33]] = [np.inf, np.nan, -np.inf]
+        w.view(np.int32)[at[31]] += 77 * p  # NaN of several bits
+    first = None
+    for _ in range(3):
+        got = policy.grad(u16(a), torch.from_numpy(w).cuda())
+        assert torch.equal(got[:, 1:], want[:, 1:])
+        assert (~torch.isfinite(got[:, 0]) | torch.isinf(t[:, 0])).all()
+        first = got if first is None else first
+        assert torch.equal(got.view(torch.int32), first.view(torch.int32))
