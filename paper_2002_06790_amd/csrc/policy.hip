@@ -1090,6 +1090,10 @@ __device__ __forceinline__ void row_weights(const float (&x)[NV], float m, float
   }
 }
 
+// (l - m) / T from 1 / T, where l - m may be beyond the largest number: half of it
+// is not, and halves are exact.
+__device__ __forceinline__ float over(float l, float m, float inv) { return __builtin_fmaf(l, 0.5f, -0.5f * m) * (2 * inv); }
+
 // A row's softmax in 32 bits.
 template <int NV>
 struct RowExp {
@@ -1100,7 +1104,7 @@ struct RowExp {
 
   // log pi of a resource with logit l: (l - m) / T is off by 2^-24 of 3 |z|.
   __device__ __forceinline__ float log_sum() const { return kLn2 * (__builtin_amdgcn_logf(sum) - shift); }
-  __device__ __forceinline__ float z(float l) const { return (l - m) * inv; }
+  __device__ __forceinline__ float z(float l) const { return over(l, m, inv); }
 };
 
 template <int G, int NV>
@@ -1777,7 +1781,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
     float sum = 0;
     uint32_t seen = 0;  // low half: entries, high half: those that found another's number
     entries([&](int k, int id, float y, float own) {
-      const float e = __builtin_amdgcn_exp2f((y - m) * row.inv * kLog2e);
+      const float e = __builtin_amdgcn_exp2f(over(y, m, row.inv) * kLog2e);
       sum += e;
       seen += entry[id] == k ? 1u : 0x10001u;
       if (own > -kInf) q[id] = e;
@@ -1797,7 +1801,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
         if (id >= a.n_res) continue;
         const float y = load_elem(top.logits, a.dtype, at_log + k);
         if (y != -kInf && load_elem(a.logits, a.dtype, at_row + id) > -kInf)
-          q[id] += __builtin_amdgcn_exp2f((y - m) * row.inv * kLog2e);
+          q[id] += __builtin_amdgcn_exp2f(over(y, m, row.inv) * kLog2e);
       }
     }
     wave_order();

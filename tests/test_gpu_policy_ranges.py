@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 import policy_ref as ref
-from test_gpu_policy import draws, host16, make_logits, mlsim, u16  # noqa: F401
+from test_gpu_policy import INF, TYPES, draws, host16, make_logits, mlsim, u16, uniform  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -161,3 +161,33 @@ def test_gradients_where_weights_that_are_not_finite_have_no_place(mlsim, shape)
         assert (~torch.isfinite(got[:, 0]) | torch.isinf(t[:, 0])).all()
         first = got if first is None else first
         assert torch.equal(got.view(torch.int32), first.view(torch.int32))
+
+
+@pytest.mark.parametrize("S", [3, 12, 900])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_logits_further_apart_than_their_type_s_largest(mlsim, dtype, S):
+    """The difference of two logits may be twice the largest number; divided by
+    a large temperature it is an ordinary exponent."""
+    x = torch.tensor([[[3e38, -3e38, 0, -INF], [-3.3e38, 3.3e38, 1e38, 2e38], [-3e38, -INF, -1e38, -2e38], [1.0, 2.0, -INF, 3.0]]]).to(TYPES[dtype])
+    rng = np.random.default_rng(S)
+    a = rng.integers(0, 4, (4, S))
+    a[:, 0] = [1, 0, 3, 0]
+    a[0, a[0] == 3], a[2, a[2] == 1], a[3, a[3] == 2] = 1, 0, 0  # allowed places
+    w = (rng.normal(size=S) * 1e10).astype(np.float32)
+    ids, y = np.array([[[0, 1, 2], [0, 1, 3], [0, 2, 3], [0, 1, 3]]]), torch.tensor([[[3e38, -3e38, 0.0]] * 4]).to(x.dtype)
+    xd, u = x.double().numpy(), uniform(rng, 4, S)
+    for T in (8e37, 3e38, 1.0):
+        policy, st = mlsim.Policy(x.cuda(), temperature=T), ref.settings_of(1, T)
+        lp, ltol = ref.logp(xd, a, st)
+        far = np.abs(lp) > 3.39e38  # beyond the largest float32, 3.403e38: the sums here are at most 3.32e38, or 4e38 and more
+        assert np.array_equal(host16(policy.sample(torch.from_numpy(u).cuda())), ref.sample(xd, u.astype(np.float64), st))
+        assert far.any() == (T == 1.0) and np.isfinite(lp).all()
+        got = policy.logp(u16(a)).cpu().numpy()
+        assert (got[far] < -3.39e38).all()
+        ref.near(got[~far], lp[~far], ltol[~far], "logp")
+        ref.near(policy.grad(u16(a), torch.from_numpy(w).cuda()).double().cpu().numpy(), *ref.grad(xd, a, w, st, dtype=dtype), "grad")
+        if T > 1:
+            loss, grad = policy.distill(u16(ids), y.cuda(), weight=torch.full((1, 4), 1e10, device="cuda"))
+            rl, lt, rg, gt = ref.distill(xd, ids, y.double().numpy(), st, np.full((1, 4), 1e10), dtype)
+            ref.near(loss.cpu().numpy(), rl, lt, "loss")
+            ref.near(grad.double().cpu().numpy(), rg, gt, "distillation's gradient")
