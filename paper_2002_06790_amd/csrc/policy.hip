@@ -1453,9 +1453,10 @@ __device__ __forceinline__ void row_grad(const RowExp<NV> &row, const float (&x)
 #pragma unroll
   for (int j = 0; j < NV; ++j) w += x[j] == -kInf ? 0.0f : h[j];
   w = group_sum<G>(w);
-  const float k = row.sum != row.sum ? row.sum : row.sum > 0 ? -w / row.sum : 0.0f;
+  const bool nan = row.sum != row.sum;
+  const float k = nan ? row.sum : row.sum > 0 ? -w / row.sum : 0.0f;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) out[j] = k != k ? k : x[j] == -kInf ? 0.0f : __builtin_fmaf(row.e[j], k, h[j]) * row.inv;
+  for (int j = 0; j < NV; ++j) out[j] = nan ? row.sum : x[j] == -kInf ? 0.0f : __builtin_fmaf(row.e[j], k, h[j]) * row.inv;
 }
 
 // Few scenarios a row (ONE: at most one): a group of lanes takes them one after
@@ -1751,6 +1752,12 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
     const int64_t at_log = pol * top.ld_log_pol + v * top.ld_log_op;
     float x[NV];
     load_spread<G, NV>(a.logits, a.dtype, at_row, g, a.n_res, x);
+    const float w = weight ? weight[row_id] : 1.0f;
+    uint32_t masked = 0;  // the logits of -inf, where the weight's product with 0 is not 0
+    if (!(fabsf(w) < kInf)) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) masked |= (uint32_t)(x[j] == -kInf) << j;
+    }
 #pragma unroll
     for (int j = 0; j < NV; j += kWords)
 #pragma unroll
@@ -1819,7 +1826,6 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
     const float nan = row.sum + (seen ? sum : 0.0f);  // NaN or not
     if (g == 0) loss[row_id] = nan != nan ? nan : l;
     if (grad.p) {
-      const float w = weight ? weight[row_id] : 1.0f;
       const float ke = nan != nan ? nan : seen && row.sum > 0 ? w / row.sum : 0.0f, kq = seen ? -w * inv : 0.0f;
       float out[NV];
 #pragma unroll
@@ -1827,6 +1833,10 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
 #pragma unroll
         for (int i = 0; i < kWords; ++i)
           out[j + i] = __builtin_fmaf(row.e[j + i], ke, q[((j / V) * G + g) * V + j % V + i] * kq) * row.inv;
+      if (masked && nan == nan) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) out[j] = masked >> j & 1 ? 0.0f : out[j];
+      }
       store_spread<G, NV>(grad.p, a.dtype, pol * grad.ld_pol + v * grad.ld_op, g, a.n_res, out);
     }
     wave_order();

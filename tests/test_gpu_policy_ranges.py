@@ -191,3 +191,29 @@ def test_logits_further_apart_than_their_type_s_largest(mlsim, dtype, S):
             rl, lt, rg, gt = ref.distill(xd, ids, y.double().numpy(), st, np.full((1, 4), 1e10), dtype)
             ref.near(loss.cpu().numpy(), rl, lt, "loss")
             ref.near(grad.double().cpu().numpy(), rg, gt, "distillation's gradient")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("P,N,R,block,S", [(4, 3, 12, 1, 4), (4, 3, 70, 1, 9), (4, 3, 40, 500, 2000), (4, 2, 600, 9000, 36000)])
+def test_weights_that_are_not_finite_leave_masked_logits_at_zero(mlsim, P, N, R, block, S, dtype):
+    """The gradient of a logit of -inf is 0 whatever the weight; an invalid row is NaN throughout."""
+    rng = np.random.default_rng(S)
+    t, x = make_logits(rng, P, N, R, dtype)
+    t[..., 0], t[..., 1] = 0.5, -INF
+    t[3, 1, 2] = float("nan")
+    masked = torch.isinf(t)
+    masked[3, 1] = False
+    a = np.zeros((N, S), np.int64)
+    pol = ref.policy_of(np.arange(S), block, 0, P)
+    w = rng.normal(size=S).astype(np.float32)
+    for p, bad in enumerate((INF, -INF, float("nan"))):
+        w[np.flatnonzero(pol == p)[0]] = bad
+    g = mlsim.Policy(t, block=block).grad(u16(a), torch.from_numpy(w).cuda())
+    assert (g[masked] == 0).all() and not torch.isfinite(g[:3][~masked[:3]]).any()
+    assert torch.isnan(g[3, 1]).all() and torch.isfinite(g[3, 0]).all()
+    ids, y = u16(np.zeros((P, N, 2))), torch.zeros((P, N, 2), dtype=t.dtype, device="cuda")
+    dw = torch.ones((P, N), device="cuda")
+    dw[0], dw[1], dw[2] = INF, -INF, float("nan")
+    loss, g = mlsim.Policy(t).distill(ids, y, weight=dw)
+    assert (g[masked] == 0).all() and not torch.isfinite(g[:3][~masked[:3]]).any()
+    assert torch.isnan(g[3, 1]).all() and torch.isfinite(g[3, 0]).all() and torch.isnan(loss[3, 1]) and torch.isfinite(loss[0]).all()
