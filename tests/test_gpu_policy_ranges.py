@@ -163,6 +163,22 @@ def test_gradients_where_weights_that_are_not_finite_have_no_place(mlsim, shape)
         assert torch.equal(got.view(torch.int32), first.view(torch.int32))
 
 
+@pytest.mark.parametrize("P,N,R,block,S", [(1, 2, 5, 1, 300_001), (2, 1, 40, 100_000, 200_003), (1, 1, 700, 1, 70_001), (3, 2, 20, 1, 30_001),
+                                           (2, 1, 600, 3, 9_001), (4, 5, 64, 700, 20_011), (1, 30, 17, 1, 16_384), (1, 3, 200, 1, 4_500_001)])
+def test_gradients_of_long_batches(mlsim, P, N, R, block, S):
+    """Sums to the grid's step: a split of the batch that is lost, or added twice, shows."""
+    rng = np.random.default_rng(S)
+    t, x = make_logits(rng, P, N, R, "float32")
+    a = draws(rng, x, S)
+    a[:, ::13] = ref.NO_PLACE
+    w = rng.normal(size=S).astype(np.float32)
+    for T in (1.0, 0.6):
+        got = mlsim.Policy(t, block=block, temperature=T).grad(u16(a), torch.from_numpy(w).cuda())
+        g, tol = ref.grad_shared(x, a, w, ref.settings_of(P, T), block)
+        ref.near(got.double().cpu().numpy(), g, tol, f"grad {P, N, R, block, S}")
+        assert ((np.abs(g) > 20 * tol) | (x == -np.inf)).mean() > 0.9  # zeros would not pass
+
+
 @pytest.mark.parametrize("S", [3, 12, 900])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_logits_further_apart_than_their_type_s_largest(mlsim, dtype, S):
