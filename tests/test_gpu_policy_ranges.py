@@ -179,6 +179,55 @@ def test_gradients_of_long_batches(mlsim, P, N, R, block, S):
         assert ((np.abs(g) > 20 * tol) | (x == -np.inf)).mean() > 0.9  # zeros would not pass
 
 
+# (policies, ops, resources): so many rows that a group of lanes takes several, for
+# every number of lanes
+EACH = [(2048, 300, 5), (4096, 130, 12), (2048, 130, 30), (1024, 70, 48), (1024, 70, 100), (1024, 34, 200), (1024, 18, 400), (1024, 18, 520),
+        (1027, 17, 1001), (1024, 16, 1024)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", EACH, ids=str)
+def test_one_draw_of_every_row(mlsim, shape, dtype):
+    P, N, R = shape
+    rng = np.random.default_rng(R)
+    t, _ = make_logits(rng, P, N, R, dtype)
+    t[3, 5] = -INF
+    t[4, 6, R // 2], t[5, 7, 0], t[6, 8, R - 1] = float("nan"), -float("nan"), INF
+    u = torch.from_numpy(uniform(rng, N, P)).cuda()
+    cuts = [dict(), dict(top_k=5), dict(temperature=0.7, top_k=8, top_p=0.9), dict(top_k=16, top_p=0.8), dict(top_p=0.9),
+            dict(top_k=20, min_p=0.02), dict(min_p=0.1, temperature=1.5), dict(temperature=0.0)]
+    cuts.append(dict(temperature=rng.choice([0.0, 0.5, 1.0, 3.0], P).astype(np.float32), top_k=rng.integers(0, R + 2, P).astype(np.float32),
+                     top_p=rng.random(P).astype(np.float32), min_p=(rng.random(P) * 0.2).astype(np.float32)))
+    for cut in cuts:
+        print(f"each {shape} {dtype} {list(cut)}", flush=True)
+        got = mlsim.Policy(t, **cut).sample(u).view(torch.int16).long() & 0xFFFF
+        want = ref.sample_each(t.double(), u.double(), torch.from_numpy(ref.settings_of(P, **cut)).cuda())
+        assert torch.equal(got, want), (cut, (got != want).nonzero()[:5])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", EACH, ids=str)
+def test_one_scenario_of_every_row(mlsim, shape, dtype):
+    """Log-probabilities and gradients; most scenarios' places are all allowed."""
+    P, N, R = shape
+    rng = np.random.default_rng(R + 1)
+    t, _ = make_logits(rng, P, N, R, dtype)
+    a = torch.from_numpy(rng.integers(0, R, (N, P))).cuda()
+    ok = torch.isfinite(t.gather(2, a.T[..., None]))[..., 0].T
+    a = torch.where(ok, a, torch.isfinite(t).float().argmax(-1).T)
+    a[2, 9], a[N - 1, 11] = R, ref.NO_PLACE
+    w = rng.normal(size=P).astype(np.float32)
+    T = rng.choice([0.5, 1.0, 3.0], P).astype(np.float32)
+    policy, place = mlsim.Policy(t, temperature=T), u16(a.cpu().numpy())
+    lp, ltol, g, gtol = ref.learn_each(t.double(), a, torch.from_numpy(w).double().cuda(), torch.from_numpy(T).double().cuda(), dtype)
+    assert torch.isfinite(lp).sum() == P - 2 and torch.isfinite(ltol[torch.isfinite(lp)]).all()
+    ref.near(policy.logp(place).cpu().numpy(), lp.cpu().numpy(), ltol.cpu().numpy(), "logp")
+    ref.near(policy.grad(place, torch.from_numpy(w).cuda()).double().cpu().numpy(), g.cpu().numpy(), gtol.cpu().numpy(), "grad")
+    few = mlsim.Policy(t[:30], temperature=T[:30])  # the same bits with fewer policies
+    assert torch.equal(few.grad(place.view(torch.int16)[:, :30].contiguous().view(torch.uint16), torch.from_numpy(w[:30]).cuda()),
+                       policy.grad(place, torch.from_numpy(w).cuda())[:30])
+
+
 @pytest.mark.parametrize("S", [3, 12, 900])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_logits_further_apart_than_their_type_s_largest(mlsim, dtype, S):
