@@ -648,7 +648,8 @@ class Graph:
         """Draw a placement for every scenario column of ``dur`` from
         ``policy`` and the random numbers ``u`` (float32 [n_ops, S]) and replay
         them (sim_policy_sample, then as ``run``).  Returns ``(makespan, finish
-        or None, status, place)``."""
+        or None, status, place)``.  On another stream than the current one,
+        ``dur`` and ``u`` are kept until they have been read."""
         import torch
         if policy.n_ops != self.n_ops or policy.n_res != self.n_res:
             raise ValueError(f"the policy is for {policy.n_ops} ops on {policy.n_res} resources, the graph has "
@@ -661,8 +662,10 @@ class Graph:
         if stream is None:  # the draw and the replay on one
             stream = torch.cuda.current_stream(policy.device)
         place = policy.sample(u, out=place, stream=stream)
-        return (*self.run(dur, place=place, want_finish=want_finish, algo=algo, stream=stream, gap=gap,
-                          delay=delay), place)
+        _, ctx = policy._on(stream, dur)
+        with ctx:  # what the replay allocates belongs to its stream too
+            return (*self.run(dur, place=place, want_finish=want_finish, algo=algo, stream=stream, gap=gap,
+                              delay=delay), place)
 
     def run_share(self, dur, share, want_finish: bool = False, makespan=None, finish=None, status=None,
                   stream=None):

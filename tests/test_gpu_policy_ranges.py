@@ -6,6 +6,7 @@ import pytest
 
 import policy_ref as ref
 from test_gpu_policy import INF, TYPES, draws, host16, make_logits, mlsim, u16, uniform  # noqa: F401
+from paper_2002_06790_amd import workloads as W
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -282,3 +283,65 @@ def test_weights_that_are_not_finite_leave_masked_logits_at_zero(mlsim, P, N, R,
     loss, g = mlsim.Policy(t).distill(ids, y, weight=dw)
     assert (g[masked] == 0).all() and not torch.isfinite(g[:3][~masked[:3]]).any()
     assert torch.isnan(g[3, 1]).all() and torch.isfinite(g[3, 0]).all() and torch.isnan(loss[3, 1]) and torch.isfinite(loss[0]).all()
+
+
+def test_run_sampled_on_another_stream(mlsim):
+    """A draw and replay on a stream that is busy, its inputs dropped at once: what
+    takes their memory does not reach the replay."""
+    w = W.make_config(1, n_scen=5000)
+    rng = np.random.default_rng(51)
+    N, S = w.n_ops, w.n_scen
+    g = mlsim.Graph.from_workload(w)
+    policy = mlsim.Policy(torch.zeros((N, w.n_res), device="cuda"))
+    dur_h, u_h = w.durations(), uniform(rng, N, S)
+    want = [q.clone() for q in g.run_sampled(policy, torch.from_numpy(dur_h).cuda(), torch.from_numpy(u_h).cuda()) if q is not None]
+    side, a = torch.cuda.Stream(), torch.ones((4096, 4096), device="cuda")
+    for _ in range(3):
+        dur, u = torch.from_numpy(dur_h).cuda(), torch.from_numpy(u_h).cuda()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                b = a @ a
+        got = [q for q in g.run_sampled(policy, dur, u, stream=side) if q is not None]
+        del dur, u
+        junk = [torch.ones((N, S), dtype=torch.int32, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        del junk, b
+        for x, y in zip(want, got):
+            assert torch.equal(x.view(torch.int16) if x.dtype == torch.uint16 else x, y.view(torch.int16) if y.dtype == torch.uint16 else y)
+    g.close()
+
+
+def test_run_sampled_captured_and_replayed(mlsim):
+    """A draw and replay in a HIP graph, with new numbers, logits and durations
+    in place, and eager calls between the replays."""
+    w = W.make_config(1, n_scen=700)
+    rng = np.random.default_rng(52)
+    N, R, S = w.n_ops, w.n_res, w.n_scen
+    g = mlsim.Graph.from_workload(w)
+    t = torch.randn((2, N, R), device="cuda")
+    policy = mlsim.Policy(t, block=100, top_p=0.9)
+    dur, u = torch.from_numpy(w.durations()).cuda(), torch.from_numpy(uniform(rng, N, S)).cuda()
+    advantage = torch.randn(S, device="cuda")
+
+    def step():
+        makespan, _, status, place = g.run_sampled(policy, dur, u)
+        return makespan, status, place.view(torch.int16), policy.logp(place), policy.grad(place, advantage)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        u.copy_(torch.from_numpy(uniform(rng, N, S)))
+        t.add_(torch.randn(t.shape, device="cuda") * 0.3)
+        dur.add_(int(rng.integers(0, 50)))
+        want = [q.clone() for q in step()]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, out)), k
+    g.close()
