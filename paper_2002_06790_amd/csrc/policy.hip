@@ -1094,6 +1094,12 @@ __device__ __forceinline__ void row_weights(const float (&x)[NV], float m, float
 // is not, and halves are exact.
 __device__ __forceinline__ float over(float l, float m, float inv) { return __builtin_fmaf(l, 0.5f, -0.5f * m) * (2 * inv); }
 
+// log2 p: the machine's logarithm takes a subnormal number for 0.
+__device__ __forceinline__ float log2_of(float p) {
+  const bool low = p < 0x1p-126f;
+  return __builtin_amdgcn_logf(low ? p * 0x1p32f : p) - (low ? 32.0f : 0.0f);
+}
+
 // A row's softmax in 32 bits.
 template <int NV>
 struct RowExp {
@@ -1820,7 +1826,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, Polic
       if (!(own > -kInf))
         l = kInf;
       else if (p > 0)
-        l += p * (kLn2 * __builtin_amdgcn_logf(p) - (row.z(own) - ls));
+        l += p * (kLn2 * log2_of(p) - (row.z(own) - ls));
     });
     l = group_sum<G>(l);
     const float nan = row.sum + (seen ? sum : 0.0f);  // NaN or not

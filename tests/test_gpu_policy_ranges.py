@@ -345,3 +345,22 @@ def test_run_sampled_captured_and_replayed(mlsim):
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(want, out)), k
     g.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("P,N,R,K,T", [(3, 40, 12, 9, 1.0), (2, 30, 108, 60, 0.1), (2, 20, 447, 18, 1.0), (1, 9, 1001, 400, 3.0)])
+def test_entries_of_a_teacher_far_apart(mlsim, P, N, R, K, T, dtype):
+    """Entries down to e^-115 of the best one: probabilities that float32 holds
+    with few bits, or not at all."""
+    rng = np.random.default_rng(R)
+    t, x = make_logits(rng, P, N, R, dtype, masked=False)
+    for twice in (False, True):
+        ids = rng.integers(0, R, (P, N, K)) if twice else np.argsort(rng.random((P, N, R)), -1)[..., :K]
+        y = torch.from_numpy(-rng.uniform(0, 115, (P, N, K)) * T)
+        y[..., 0] = 0
+        y = y.to(TYPES[dtype])
+        policy, st = mlsim.Policy(t, temperature=T), ref.settings_of(P, T)
+        loss, grad = policy.distill(u16(ids), y.cuda())
+        rl, lt, rg, gt = ref.distill(x, ids, y.double().numpy(), st, None, dtype)
+        ref.near(loss.cpu().numpy(), rl, lt, "loss")
+        ref.near(grad.double().cpu().numpy(), rg, gt, "grad")
