@@ -353,11 +353,16 @@ class Policy:
 
     ``temperature``, ``top_k`` (0: all), ``top_p`` and ``min_p``: numbers, or
     one per policy as a sequence or tensor (rounded to float32; tensors on the
-    GPU are copied on the current stream).  Only ``sample`` reads the last three.
+    GPU are copied on the current stream).  Only ``sample`` reads the last
+    three: ``logp`` and ``grad`` are of the probabilities before any cut, so for
+    placements drawn with one, ``grad`` of their costs is no unbiased estimate
+    of the cost's gradient.
 
     Calls run on ``stream`` (default: the current stream of the logits'
-    device), are asynchronous and may be captured into a graph.  Gradients come
-    back as tensors: ``logits.backward(policy.grad(...))`` hands them on to a
+    device), are asynchronous and may be captured into a graph.  Nothing is
+    recorded for autograd, also for logits that require a gradient: ``logp``
+    and ``distill`` return plain tensors, gradients come from ``grad`` and
+    ``distill``, and ``logits.backward(policy.grad(...))`` hands them on to a
     network that made the logits.
     """
 
