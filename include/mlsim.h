@@ -475,9 +475,9 @@ int sim_policy_sample(const sim_policy *p, int64_t n_scen, const float *u, int64
 
 /*
  * logp[s] (device float32 [n_scen]) = the sum over the ops of the logarithm of
- * the probability of place[v][s] in its row (top_k, top_p and min_p are not
- * read: it is the probability before any cut).  -inf where an op's place is >= n_res or its logit -inf (every place
- * of an empty row); NaN where a row is invalid or T = 0.
+ * the probability of place[v][s] in its row before any cut (top_k, top_p and
+ * min_p are not read).  -inf where an op's place is >= n_res or its logit -inf
+ * (every place of an empty row); NaN where a row is invalid or T = 0.
  *   work, work_bytes  device scratch of at least sim_policy_work bytes (the same
  *          for logp and grad; 0: may be NULL), aligned to 8, for this call alone
  *          until it has run.

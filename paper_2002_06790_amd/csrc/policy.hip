@@ -1,7 +1,9 @@
 // Placement policies: rows of logits over resources, one row per op and
 // policy.  A group of G lanes (1 to 64) holds a row, NV resources a lane (8, or 16
 // beyond 512 resources), so that up to 64 rows share a wavefront and the sums
-// within a row take log2 G exchanges.  Times beside the kernels are of one MI355X.
+// within a row take log2 G exchanges.  Times beside the kernels are of one MI355X,
+// of calls between others: the same call again and again for some milliseconds
+// slows the card down, by a third for the longest draws.
 #include <algorithm>
 #include <climits>
 
@@ -889,12 +891,15 @@ struct RowWalk {
 };
 
 // One scenario a row at most: a group of lanes works a row out in 32 bits and
-// draws.  A draw that lies within the roundings of a border (about one in a
-// thousand at 64 resources) is done again in 64 bits by the whole wavefront, so
-// that every answer is the 64-bit one.  Bound by vector instructions: 1024 x 6624
-// rows of 48 bf16 take 0.26 ms uncut and 0.41 ms with top_k 8 and top_p 0.9 (the
-// eight largest of two rows at once, the next two already loading; 0.54 ms with a
-// sort for each, 3.5 ms with all sums in 64 bits and the cut searched bit by bit).
+// draws.  A draw that lies within the roundings of a border (63 borders at 64
+// resources, 2^-16 of the sum to either side: two in a thousand) is done again in
+// 64 bits by the whole wavefront, so that every answer is the 64-bit one.  Bound
+// by vector instructions: 1024 x 6624 rows of 48 bf16 take 0.26 ms uncut and 0.41
+// ms with top_k 8 and top_p 0.9 (the eight largest of two rows at once, the next
+// two already loading; 316 instructions a row and wavefront, 4 clocks each, are all
+// of the time; 0.54 ms with a sort for each, 3.5 ms with all sums in 64 bits and the
+// cut searched bit by bit).  The registers of the 64-bit way count for the whole
+// kernel: rows of over 512 resources run two wavefronts a SIMD.
 template <int G, int NV, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_one(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
                                                                 uint16_t *place, int64_t ld_place, Tile t,
@@ -1014,7 +1019,7 @@ struct PolicyScenarios {
 // length steps down the sums, sure where both neighbours of the place found are
 // more than the margin away (sums that the roundings put out of order are
 // nearer to each other than that).  12 x 6624 rows of 48 bf16, cut, 32 draws each:
-// 37 us.
+// 32 us.
 template <int G, int NV, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_policy_sample_few(PolicyArgs a, int64_t n_scen, const float *u, int64_t ld_u,
                                                                 uint16_t *place, int64_t ld_place, Tile t,
@@ -1249,7 +1254,9 @@ __device__ __forceinline__ Piece piece_of(const PolicyArgs &a, const Pieces &ps,
 // of as many rows as it has groups of lanes into LDS, then every thread adds up
 // its scenarios' entries, one 16-byte load of eight places per row.  Entry
 // n_res stands for a place that is no resource.  Bound by memory (the times stand
-// at logp_runs).
+// at logp_runs).  32 terms are added in 32 bits, the rest in 64, and a chunk's sum
+// is rounded once for the join: no term is above 0, so that each rounding is off by
+// 2^-24 of the whole sum at most, as the result's own is.
 template <int G, int NV, int E>
 __global__ __launch_bounds__(kThreads) void k_policy_logp_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
                                                                int64_t ld_place, float *part, Pieces ps, int ops_per,
@@ -1452,7 +1459,8 @@ __global__ __launch_bounds__(kThreads) void k_policy_sample_runs(PolicyArgs a, i
   }
 }
 
-// The gradient of a row from its softmax and what every resource received.
+// The gradient of a row from its softmax and what every resource received.  T
+// divides last: at 2^-126 a product before it would be infinite.
 template <int G, int NV>
 __device__ __forceinline__ void row_grad(const RowExp<NV> &row, const float (&x)[NV], const float (&h)[NV], float (&out)[NV]) {
   float w = 0;
@@ -1569,7 +1577,7 @@ struct GradShape {
 // with 4; one of float32 takes 193, 3 a lane.)  Then a wavefront adds up a row's
 // columns and goes on to its gradient.  With several splits of the batch a row's
 // sums go to `part`, and the next kernel joins them.  Bound by memory: 20000 rows
-// of 64, 16384 scenarios each, take 125 us with the weights' peak, 5.3 TB/s; with
+// of 64, 16384 scenarios each, take 126 us with the weights' peaks, 5.3 TB/s; with
 // a row a block 176, without the grid (columns for half a wavefront) 228.
 template <int NV, int WR>
 __global__ __launch_bounds__(kThreads) void k_policy_grad_runs(PolicyArgs a, int64_t n_scen, const uint16_t *place,
@@ -1739,7 +1747,7 @@ __global__ __launch_bounds__(kThreads) void k_policy_grad_join(PolicyArgs a, con
 // gradient is 0 and it makes the loss infinite.  Entries that share a resource are
 // found by writing every entry's number to its resource and reading it back;
 // one lane then adds them up in order.  Bound by memory: 16 x 20000 rows of 1001
-// float32 with 32 entries take 489 us, 5.4 TB/s.
+// float32 with 32 entries take 486 us, 5.4 TB/s.
 template <int G, int NV>
 __global__ __launch_bounds__(kThreads) void k_policy_distill(PolicyArgs a, PolicyTop top, const float *weight,
                                                              float *loss, PolicyOut grad, int64_t rows) {
@@ -1948,8 +1956,8 @@ int64_t make_pieces(const PolicyArgs &a, int64_t n_scen, int64_t span, Pieces &p
 
 // Whether a row's table is worth making: the row kernel works through a whole
 // row for every scenario, a table costs that twice and as much as 48 lanes more.
-// 1024 scenarios of 6624 rows of 48, 4 and 8 a table: 231 and 131 us, row by row
-// 138 and 134; 4096 of 8, 16 a table: 251 us, row by row 93.
+// 1024 scenarios of 6624 rows of 48 bf16, 4 and 8 a table: 230 and 131 us, row by
+// row 127 and 124; 4096 of 8, 16 a table: 253 us, row by row 60.
 bool long_runs(const PolicyArgs &a, int64_t n_scen) {
   const int64_t lanes = row_lanes(a.n_res);
   return std::min(a.block, n_scen) * lanes > 2 * lanes + 48;
@@ -1960,9 +1968,9 @@ constexpr double kPerUs = 600e3;  // wavefront instructions of all SIMDs in a mi
 // Whether the draws go row by row by groups of lanes, or a wavefront a row and
 // run: by the instructions of either, and by their latency where there are few
 // rows.  A group works a row out in about 300 and takes 200 for every G draws; a
-// wavefront in 64 bits in 450.  2000000 rows of 64, 63 draws each: 784 us by
-// groups, 1470 by wavefronts; 256 draws: 1474 by wavefronts; 17403 rows of 4, 47
-// draws: 32 us by groups (47 rounds one after another), 13 by wavefronts.
+// wavefront in 64 bits in 450.  2000000 rows of 64, 63 draws each: 1010 us by
+// groups, 1480 by wavefronts; 256 draws: 3650 and 1480; 17403 rows of 4, 47 draws:
+// 30 us by groups (47 rounds one after another), 13 by wavefronts.
 bool sample_by_rows(const PolicyArgs &a, int64_t n_scen) {
   const int64_t run = std::min(a.block, n_scen), lanes = row_lanes(a.n_res);
   const double rows = (double)a.n_pol * a.n_ops, rounds = (double)((std::max(n_scen / a.n_pol, run) + lanes - 1) / lanes);
@@ -1974,8 +1982,9 @@ bool sample_by_rows(const PolicyArgs &a, int64_t n_scen) {
 
 // Whether a gradient's scenarios are added by groups of lanes in registers (38
 // instructions each) or by a wavefront a row in LDS (about 480 a row, twice that for
-// the longest).  2000000 rows of 64: with 16, 32 and 63 scenarios a row 450, 658 and 1118 us
-// by groups, 1540 to 1664 by wavefronts; 127620 rows of 149 with 57: 233 us, and 111.
+// the longest).  2000000 rows of 64 bf16: with 16, 32 and 63 scenarios a row 393, 597
+// and 1104 us by groups, 1770 to 1850 by wavefronts; 127620 rows of 149 with 57: 237
+// us, and 106.
 bool grad_by_rows(const PolicyArgs &a, int64_t n_scen) {
   const double lanes = row_lanes(a.n_res), rows = (double)a.n_pol * a.n_ops, long_row = a.n_res > 512 ? 2.3 : 1;
   const double scen = (double)std::max(n_scen / a.n_pol, std::min(a.block, n_scen));
