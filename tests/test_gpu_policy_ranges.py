@@ -364,3 +364,18 @@ def test_entries_of_a_teacher_far_apart(mlsim, P, N, R, K, T, dtype):
         rl, lt, rg, gt = ref.distill(x, ids, y.double().numpy(), st, None, dtype)
         ref.near(loss.cpu().numpy(), rl, lt, "loss")
         ref.near(grad.double().cpu().numpy(), rg, gt, "grad")
+
+
+def test_gradients_where_one_policy_has_all_scenarios(mlsim):
+    """A thousand policies and a block longer than the batch: one policy's sums
+    to the grid's step, zeros for the others."""
+    P, N, R, S = 1000, 2, 5, 200_000
+    rng = np.random.default_rng(61)
+    t, x = make_logits(rng, P, N, R, "float32")
+    for scen0 in (0, 7 * 10**9 - 50_000):
+        a = draws(rng, x[ref.policy_of(np.arange(0, S, S - 1), 10**9, scen0, P)], S)
+        w = (rng.normal(size=S) * 100).astype(np.float32)
+        got = mlsim.Policy(t, block=10**9, scen0=scen0).grad(u16(a), torch.from_numpy(w).cuda())
+        g, tol = ref.grad_shared(x, a, w, ref.settings_of(P), 10**9, scen0)
+        ref.near(got.double().cpu().numpy(), g, tol, "grad")
+        assert (np.abs(g) > 20 * tol).any((1, 2)).sum() == (1 if scen0 == 0 else 2)
